@@ -93,7 +93,15 @@ __device__ __forceinline__ bool ring_fill(Ring& ring, RingPlace& at, int stages,
     at.next(stages);
     return true;
 }
-// ... and before it leaves: no copy may still be under way.  `at` is where the next fill would have gone.
+// A taking warp, whole, has read the stage it is at.  The copy that comes next writes through another proxy than the one that the
+// warp read through: without the fence a read that still waits (behind a queue of scattered stores, say) may find that copy's data.
+__device__ __forceinline__ void ring_release(Ring& ring, RingPlace& at, int stages) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) barrier_arrive(&ring.empty[at.stage]);
+    at.next(stages);
+}
+// The filling thread, before it leaves: no copy may still be under way.  `at` is where the next fill would have gone.
 __device__ __forceinline__ void ring_drain(Ring& ring, const RingPlace& at, int stages, const BoundedWait& wait) {
     for (int i = 0; i < stages; ++i) {
         const bool this_round = i < at.stage;

@@ -88,9 +88,7 @@ __device__ __forceinline__ bool take_row(StreamShared& s, const Slot& slot, cons
             for (int j = 0; j < kTake; ++j)
                 q[j] = k + j * kTakers < row.count ? in[j * kTakers] : make_uint4(ninf, ninf, ninf, ninf);
         }
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) barrier_arrive(&s.ring.empty[at.stage]);
-        at.next(stage_count);
+        ring_release(s.ring, at, stage_count);
         work(q, k, flag);
     }
     return true;

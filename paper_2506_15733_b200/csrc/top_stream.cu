@@ -347,9 +347,7 @@ __device__ __forceinline__ bool take_row(StreamShared& s, const uint8_t* stages,
                 q[j] = base + k < row.count ? in[k] : make_uint4(ninf, ninf, ninf, ninf);
             }
         }
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) barrier_arrive(&s.ring.empty[at.stage]);
-        at.next(stage_count);
+        ring_release(s.ring, at, stage_count);
         out.add_pairs(q, now, want_sum);
         if (--left == 0 || base + kStageUnits >= row.count) {
             out.set_pair(turn++, now);
