@@ -23,10 +23,12 @@ enum { kForward, kBackward, kStep };
 
 // A part of a row.  Student, over some of the logits: the largest, sums of exp((l - top) / T) over all and over the
 // unlisted entries.  Teacher, over its share of the list: sums of e_j = exp(a_j - ref) and of
-// e_j ((a_j - ref) - (b_j - near / T)).
-struct Part { float top, all, rest, near; double ref, mass, cross; };
+// e_j ((a_j - ref) - (b_j - near / T)), the latter without entries that the student rules out (b_j = -inf): of those the largest
+// t_j is kept, `lost`.  They make the loss infinite where q_j > 0 and are nothing where q_j = 0, which only the row's norm tells: a
+// share of negligible entries has e_j = 1 all the same.
+struct Part { float top, all, rest, near, lost; double ref, mass, cross; };
 
-__device__ __forceinline__ Part no_part() { return {-INFINITY, 0.0f, 0.0f, 0.0f, -INFINITY, 0.0, 0.0}; }
+__device__ __forceinline__ Part no_part() { return {-INFINITY, 0.0f, 0.0f, 0.0f, -INFINITY, -INFINITY, 0.0, 0.0}; }
 
 // The row's: the student's as above, and norm, sum of q_j (`listed`) and q_r (`left`) of the teacher.
 struct Row { float top, sum, rest, left; double norm, listed; };
@@ -66,10 +68,12 @@ __device__ __forceinline__ void combine_student(const DistillArgs& a, const Part
 // One warp: the row's loss, in lane 0.
 __device__ __forceinline__ float row_loss(const DistillArgs& a, const Part& p, const Row& row) {
     const double ln_sum = log((double)row.sum);
+    const bool none = row.top == -INFINITY && row.sum == 0.0f;      // a student without any entry: all that is listed is lost
+    const double share = p.mass != 0.0 ? exp(p.ref - row.norm) : 0.0;
     double loss = 0.0;
-    if (p.mass != 0.0)                                     // a student without any entry gives the listed ones nothing
-        loss = row.top == -INFINITY && row.sum == 0.0f ? INFINITY
-             : exp(p.ref - row.norm) * (p.cross + p.mass * ((p.ref - row.norm) - ((double)p.near - (double)row.top) * (double)a.inv_t + ln_sum));
+    if (share != 0.0 && !none)
+        loss = share * (p.cross + p.mass * ((p.ref - row.norm) - ((double)p.near - (double)row.top) * (double)a.inv_t + ln_sum));
+    if (p.lost != -INFINITY && exp((double)p.lost * (double)a.inv_t - row.norm) > 0.0) loss += INFINITY;
     loss = warp_reduce(loss, AddOp());
     if (row.left > 0.0f && row.rest > 0.0f)
         loss += (double)row.left * (log((double)row.left) - (log((double)row.rest) - ln_sum));

@@ -82,14 +82,18 @@ __device__ void list_sums(const DistillArgs& a, int64_t r, const T* row, int sha
     part.near = near == -INFINITY ? 0.0f : near;
     part.ref = a.top_lse ? (double)a.top_lse[r] : (double)most * (double)a.inv_t;
     part.mass = part.cross = 0.0;
+    part.lost = -INFINITY;
     for (int j = first; j < a.K; j += step) {
         const int id = ids[j];
         if (id < 0 || id >= a.V || t[j] == -INFINITY) continue;
         const double x = (double)t[j] * (double)a.inv_t - part.ref, e = exp(x);
         part.mass += e;
-        if (logits && e != 0.0)
-            part.cross += e * (x - ((double)Elem<T>::to_float(row[id]) - (double)part.near) * (double)a.inv_t);
+        if (!logits || e == 0.0) continue;
+        const float logit = Elem<T>::to_float(row[id]);
+        if (logit == -INFINITY) part.lost = fmaxf(part.lost, t[j]);
+        else part.cross += e * (x - ((double)logit - (double)part.near) * (double)a.inv_t);
     }
+    part.lost = warp_reduce(part.lost, MaxOp());
     part.mass = warp_reduce(part.mass, AddOp());
     part.cross = warp_reduce(part.cross, AddOp());
 }

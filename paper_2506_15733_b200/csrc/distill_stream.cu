@@ -207,9 +207,11 @@ __device__ void load_list(const DistillArgs& a, int64_t r, Slot& slot, uint32_t*
         if (id[i] < 0 || value[i] == -INFINITY) continue;
         const double x = (double)value[i] * (double)a.inv_t - part.ref, e = exp(x);
         part.mass += e;
-        if (kMode != kBackward && e != 0.0)
-            part.cross += e * (x - ((double)logit[i] - (double)part.near) * (double)a.inv_t);
+        if (kMode == kBackward || e == 0.0) continue;
+        if (logit[i] == -INFINITY) part.lost = fmaxf(part.lost, value[i]);
+        else part.cross += e * (x - ((double)logit[i] - (double)part.near) * (double)a.inv_t);
     }
+    part.lost = warp_reduce(part.lost, MaxOp());
     part.mass = warp_reduce(part.mass, AddOp());
     part.cross = warp_reduce(part.cross, AddOp());
     if (lane == 0) slot.part[warp] = part;
