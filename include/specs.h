@@ -460,7 +460,8 @@ int specs_top_logits(specs_ctx* ctx, const void* logits, int dtype, int64_t row_
  *   q_j  = exp(t_j / T - top_lse)             with top_lse float [rows], the teacher's own ln sum exp(. / T) as
  *                                             specs_top_logits gives it at the same T
  *   q_r  = max(0, 1 - sum_j q_j)              what the list leaves out, held against p_r, what p has outside the list
- *          (0 where p_r = 0)
+ *          (0 where p_r = 0, or where every logit outside the list lies more than 690 T below the row's largest: such
+ *          masks leave p_r below 1e-300)
  *   or, with top_lse == NULL, q = softmax of the list's t / T and q_r = 0;
  *   loss = row_weight * [ sum_j q_j (ln q_j - ln p_{id_j}) + q_r (ln q_r - ln p_r) ]
  *   grad = grad_loss * row_weight / T * { p_v S - sum of q_j with id_j = v   for a listed id v
@@ -472,7 +473,8 @@ int specs_top_logits(specs_ctx* ctx, const void* logits, int dtype, int64_t row_
  *   row_weight, grad_loss float [rows] or NULL (1).  A row of weight 0 is not read: loss 0, gradient 0.
  *   stats                float [rows, 3]: the row's largest logit, sum_v exp((l_v - largest) / T), and the part of
  *                        that sum outside the list (0 without top_lse; all 0 for a row of weight 0 or with a bad
- *                        id).  Written by the forward pass (may be NULL there), read by the backward pass.
+ *                        id).  Where that part is below 2^-126 its natural logarithm stands in its place, which is
+ *                        negative.  Written by the forward pass (may be NULL there), read by the backward pass.
  *   grad_logits          [rows, V] out of the logits' dtype, rows grad_stride >= V elements apart, rounded to nearest
  *                        from fp32.  May be `logits` itself (with the same stride), never another overlap.
  * specs_distill_step is forward and backward in one pass over the logits, for a training step whose

@@ -7,9 +7,9 @@
 //   dKL/dl_v = (p_v S - sum of q_j with id_j = v) / T   for a listed id v,    S = sum_j q_j + q_r
 //            = p_v (S - q_r / p_r) / T                  elsewhere
 //
-// p_r is summed over the entries that are not listed, not taken as 1 - the others: a student that is sure of a
-// listed word leaves a p_r far below the rounding of 1.  Membership is a bit per element in shared memory.
-//
+// p_r is summed over the entries that are not listed, not taken as 1 - the others, and relative to the largest of them, not
+// of the row: a student that is sure of a listed word leaves a p_r far below the rounding of 1, and below the range of a float.
+// Where the largest unlisted logit lies more than kLeastRest T below the row's largest, p_r counts as 0.
 //
 // This header has the arithmetic that the kernels share; distill_rows.cu the kernel for few rows, distill_stream.cu the one for
 // many.
@@ -21,17 +21,25 @@ namespace specs {
 
 enum { kForward, kBackward, kStep };
 
-// A part of a row.  Student, over some of the logits: the largest, sums of exp((l - top) / T) over all and over the
-// unlisted entries.  Teacher, over its share of the list: sums of e_j = exp(a_j - ref) and of
-// e_j ((a_j - ref) - (b_j - near / T)), the latter without entries that the student rules out (b_j = -inf): of those the largest
-// t_j is kept, `lost`.  They make the loss infinite where q_j > 0 and are nothing where q_j = 0, which only the row's norm tells: a
-// share of negligible entries has e_j = 1 all the same.
-struct Part { float top, all, rest, near, lost; double ref, mass, cross; };
+// A part of a row.  Student, over some of the logits: the largest unlisted one, `top`, and the sum of exp((l - top) / T) over
+// the unlisted ones; the largest listed one, `near`, and the sum over those (each id once) relative to it.  Without a normaliser
+// (top_lse) nothing is held against the remaining mass, and all logits count as unlisted.
+// Teacher, over its share of the list: sums of e_j = exp(a_j - ref) and of e_j ((a_j - ref) - (b_j - near / T)), the latter
+// without entries that the student rules out (b_j = -inf): of those the largest t_j is kept, `lost`.  They make the loss infinite
+// where q_j > 0 and are nothing where q_j = 0, which only the row's norm tells: a share of negligible entries has e_j = 1 all the
+// same.
+struct Part { float top, rest, near, listed, lost; double ref, mass, cross; };
 
-__device__ __forceinline__ Part no_part() { return {-INFINITY, 0.0f, 0.0f, 0.0f, -INFINITY, -INFINITY, 0.0, 0.0}; }
+__device__ __forceinline__ Part no_part() { return {-INFINITY, 0.0f, -INFINITY, 0.0f, -INFINITY, -INFINITY, 0.0, 0.0}; }
+__device__ __forceinline__ float finite_or_zero(float v) { return v == -INFINITY ? 0.0f : v; }
 
-// The row's: the student's as above, and norm, sum of q_j (`listed`) and q_r (`left`) of the teacher.
-struct Row { float top, sum, rest, left; double norm, listed; };
+// The row's.  Student: the largest logit, the sum over all entries relative to it, and of that the unlisted part (which may have
+// underflowed); the largest unlisted logit, and the sum over the unlisted ones relative to it.  Teacher: norm, the sum of q_j
+// (`listed`), and q_r where it counts (`left`).
+struct Row { float top, sum, rest, rest_top, rest_own, left; double norm, listed; };
+
+constexpr double kLeastRest = 690.0;                       // exp() of it: 1e-300, well inside the range of a double
+constexpr float kNearRest = 1e-17f;                        // `rest` from here on: fp32 relative to the row's largest logit will do
 
 // q_j for the gradient: the exponent in 64 bits, rounded once.
 __device__ __forceinline__ float teacher_q(float t, float inv_t, double norm) {
@@ -57,12 +65,46 @@ __device__ __forceinline__ void combine_teacher(const DistillArgs& a, const Part
         row.left = 0.0f;
     }
 }
-// ... and the student.
-__device__ __forceinline__ void combine_student(const DistillArgs& a, const Part& p, float c, Row& row) {
-    row.top = warp_reduce(p.top, MaxOp());
-    const double f = p.top == -INFINITY || p.top == row.top ? 1.0 : (double)fast_exp2((p.top - row.top) * c);
-    row.sum = (float)warp_reduce((double)p.all * f, AddOp());
-    row.rest = a.top_lse ? (float)warp_reduce((double)p.rest * f, AddOp()) : 0.0f;
+// What takes a sum of exponentials relative to one logit to another, larger one.
+__device__ __forceinline__ float moved(float from, float to, float c) {
+    return from == -INFINITY || from == to ? 1.0f : fast_exp2((from - to) * c);
+}
+// ... the student's listed entries, over all parts: the largest, and the sum relative to it ...
+struct Listed { float near, sum; };
+__device__ __forceinline__ Listed combine_listed(const Part& p, float c) {
+    const float near = warp_reduce(p.near, MaxOp());
+    return {near, (float)warp_reduce((double)p.listed * moved(p.near, near, c), AddOp())};
+}
+// ... and the student with these.
+__device__ __forceinline__ void combine_student(const DistillArgs& a, const Part& p, const Listed& listed, float c, Row& row) {
+    row.rest_top = warp_reduce(p.top, MaxOp());
+    row.rest_own = (float)warp_reduce((double)p.rest * moved(p.top, row.rest_top, c), AddOp());
+    row.top = fmaxf(row.rest_top, listed.near);            // (without top_lse all of these are in rest_top, and listed.sum is 0)
+    row.rest = row.rest_own * moved(row.rest_top, row.top, c);
+    row.sum = row.rest + listed.sum * moved(listed.near, row.top, c);
+    if (!(row.rest_own > 0.0f) || ((double)row.top - (double)row.rest_top) * (double)a.inv_t > kLeastRest) row.left = 0.0f;
+}
+
+// What the forward pass leaves of the unlisted part for the backward pass: itself, or its logarithm where it is below the normal
+// floats (which is negative, while it is not); 0 where it does not count.
+__device__ __forceinline__ float rest_to_stats(const DistillArgs& a, const Row& row) {
+    const double down = ((double)row.rest_top - (double)row.top) * (double)a.inv_t;
+    if (!a.top_lse || row.rest_own == 0.0f || down < -kLeastRest) return 0.0f;
+    const double rest = (double)row.rest_own * exp(down);
+    return rest < 1.1754943508222875e-38 ? (float)(log((double)row.rest_own) + down) : (float)rest;
+}
+__device__ __forceinline__ void student_from_stats(const DistillArgs& a, int64_t r, Row& row) {
+    row.top = row.rest_top = a.stats[3 * r];
+    row.sum = a.stats[3 * r + 1];
+    const float rest = a.stats[3 * r + 2];
+    row.rest = row.rest_own = fmaxf(rest, 0.0f);
+    if (!(rest != 0.0f) || rest != rest) {
+        row.left = 0.0f;
+    } else if (rest < kNearRest) {                         // relative to a logit about as large as the largest unlisted one
+        const double ln_rest = rest < 0.0f ? (double)rest : log((double)rest);
+        row.rest_top = (float)((double)row.top + ln_rest / (double)a.inv_t);
+        row.rest_own = (float)exp(ln_rest - ((double)row.rest_top - (double)row.top) * (double)a.inv_t);
+    }
 }
 
 // One warp: the row's loss, in lane 0.
@@ -72,20 +114,38 @@ __device__ __forceinline__ float row_loss(const DistillArgs& a, const Part& p, c
     const double share = p.mass != 0.0 ? exp(p.ref - row.norm) : 0.0;
     double loss = 0.0;
     if (share != 0.0 && !none)
-        loss = share * (p.cross + p.mass * ((p.ref - row.norm) - ((double)p.near - (double)row.top) * (double)a.inv_t + ln_sum));
+        loss = share * (p.cross + p.mass * ((p.ref - row.norm) -
+                                             ((double)finite_or_zero(p.near) - (double)row.top) * (double)a.inv_t +
+                                             ln_sum));
     if (p.lost != -INFINITY && exp((double)p.lost * (double)a.inv_t - row.norm) > 0.0) loss += INFINITY;
     loss = warp_reduce(loss, AddOp());
-    if (row.left > 0.0f && row.rest > 0.0f)
-        loss += (double)row.left * (log((double)row.left) - (log((double)row.rest) - ln_sum));
+    if (row.left > 0.0f)
+        loss += (double)row.left * (log((double)row.left) - (log((double)row.rest_own) +
+                                                             ((double)row.rest_top - (double)row.top) * (double)a.inv_t - ln_sum));
     return (float)loss;
 }
 
-// A thread's running sums of 2^((l - top) c), up to the exponents' common error: over listed entries and over the
-// others.  Where nothing but -inf (and NaN) has been seen the exponentials are taken from 0, which makes them 0 (NaN).
+// A unit without the elements whose bits are set: they become -inf.
+template <typename T>
+__device__ __forceinline__ void hide(uint4& q, uint32_t bits) {
+    constexpr int kPerWord = 4 / sizeof(T);
+    uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t mask;
+        if (kPerWord == 1) mask = (bits >> i) & 1u ? 0xffffffffu : 0u;
+        else mask = ((bits >> (2 * i)) & 1u ? 0xffffu : 0u) | ((bits >> (2 * i + 1)) & 1u ? 0xffff0000u : 0u);
+        w[i] = (w[i] & ~mask) | (Elem<T>::kNegInfWord & mask);
+    }
+    q = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// A thread's running sum of 2^((l - top) c) over unlisted entries, up to the exponents' common error.  Where nothing but -inf
+// (and NaN) has been seen the exponentials are taken from 0, which makes them 0 (NaN).
 template <typename T>
 struct RunningSums {
     static constexpr int kPairs = Elem<T>::kWidth / 2;
-    float c, top = -INFINITY, listed = 0.0f;
+    float c, top = -INFINITY;
     float2 rest = make_float2(0.0f, 0.0f);
     Exponent ex;
     __device__ explicit RunningSums(float c_) : c(c_), ex(0.0f, c_) {}
@@ -94,55 +154,56 @@ struct RunningSums {
         if (most > top) {
             if (top != -INFINITY) {
                 const float scale = fast_exp2((top - most) * c) * ex.mend;
-                listed *= scale;
                 rest = __fmul2_rn(rest, make_float2(scale, scale));
             }
             top = most;
             ex = Exponent(top, c);
         }
     }
-    // kUnits units; flagged(j): unit j may have listed entries, which bits_of(j) then has as a mask.
+    // kUnits units, which are changed; flagged(j): unit j may have listed entries, which bits_of(j) then has as a mask.
     template <int kUnits, typename Flagged, typename BitsOf>
-    __device__ __forceinline__ void add(const uint4* q, const Flagged& flagged, const BitsOf& bits_of) {
+    __device__ __forceinline__ void add(uint4* q, const Flagged& flagged, const BitsOf& bits_of) {
+        bool any = false;
+#pragma unroll
+        for (int j = 0; j < kUnits; ++j) any |= flagged(j);
+        if (any) {
+#pragma unroll
+            for (int j = 0; j < kUnits; ++j)
+                if (flagged(j)) hide<T>(q[j], bits_of(j));
+        }
         raise(units_max<T, kUnits>(q, top));
 #pragma unroll
         for (int j = 0; j < kUnits; ++j) {
             float2 e[kPairs];
             ex.of_unit<T>(q[j], e);
-            if (flagged(j)) {
-                const uint32_t bits = bits_of(j);
 #pragma unroll
-                for (int k = 0; k < kPairs; ++k) {
-                    const bool x = (bits >> (2 * k)) & 1u, y = (bits >> (2 * k + 1)) & 1u;
-                    listed += (x ? e[k].x : 0.0f) + (y ? e[k].y : 0.0f);
-                    e[k] = make_float2(x ? 0.0f : e[k].x, y ? 0.0f : e[k].y);
-                }
-            }
-            float2 sum = e[0];
-#pragma unroll
-            for (int k = 1; k < kPairs; ++k) sum = __fadd2_rn(sum, e[k]);
-            rest = __fadd2_rn(rest, sum);
+            for (int k = 1; k < kPairs; ++k) e[0] = __fadd2_rn(e[0], e[k]);
+            rest = __fadd2_rn(rest, e[0]);
         }
     }
-    // The warp's sums, in every lane.
+    // The warp's, in every lane.
     __device__ __forceinline__ void of_warp(Part& part) const {
         part.top = warp_reduce(top, MaxOp());
         const float scale = top == -INFINITY ? 1.0f : fast_exp2((top - part.top) * c) * ex.mend;
         part.rest = warp_reduce((rest.x + rest.y) * scale, AddOp());
-        part.all = part.rest + warp_reduce(listed * scale, AddOp());
     }
 };
 
-// What makes the gradient of an entry from its logit.
+// What makes the gradient of an entry from its logit: of an unlisted one rest 2^exponent, the exponent relative to the row's largest
+// logit, or to the largest unlisted one where that is so far below it that its powers would underflow.  (Listed entries may
+// overflow then; they get their own gradient.)
 struct Gradient {
     Exponent ex;
-    float inv_sum, S, rest;                                // of an unlisted entry: rest 2^exponent
-    float scale;
-    __device__ Gradient(const Row& row, float c, float scale_) : ex(row.top == -INFINITY ? 0.0f : row.top, c), scale(scale_) {
-        inv_sum = row.sum == 0.0f ? 0.0f : ex.mend / row.sum;
-        const float left = row.rest > 0.0f ? row.left : 0.0f;
-        S = (float)row.listed + left;
-        rest = scale * inv_sum * (left > 0.0f ? S - left * (row.sum / row.rest) : S);
+    float rest, top, inv_sum, S, scale;
+    __device__ Gradient(const Row& row, float c, float scale_) : ex(0.0f, c), scale(scale_) {
+        top = finite_or_zero(row.top);
+        const bool far = row.left > 0.0f && !(row.rest >= kNearRest);
+        const float ref = far ? row.rest_top : top;
+        ex = Exponent(ref, c);
+        inv_sum = row.sum == 0.0f ? 0.0f : 1.0f / row.sum;
+        S = (float)row.listed + row.left;
+        const float share = row.left > 0.0f ? row.left / (far ? row.rest_own : row.rest) : 0.0f;
+        rest = scale * (ex.mend * (S * inv_sum * moved(ref, top, c) - share));
     }
     template <typename T>
     __device__ __forceinline__ uint4 unit(const uint4& q) const {
@@ -151,6 +212,10 @@ struct Gradient {
 #pragma unroll
         for (int i = 0; i < Elem<T>::kWidth / 2; ++i) e[i] = __fmul2_rn(e[i], make_float2(rest, rest));
         return Elem<T>::narrow(reinterpret_cast<const float*>(e));
+    }
+    __device__ __forceinline__ float unlisted(float logit) const { return rest * ex.of_logit(logit); }
+    __device__ __forceinline__ float listed(float logit, float q) const {
+        return scale * (fast_exp2((logit - top) * ex.c) * inv_sum * S - q);
     }
 };
 

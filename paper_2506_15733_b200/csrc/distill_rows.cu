@@ -33,7 +33,7 @@ __host__ __device__ constexpr int padded_units(int count) {
 
 struct Shared {
     Part part[kMaxCluster];
-    float top[kStreamWarps], all[kStreamWarps], rest[kStreamWarps];
+    float top[kStreamWarps], rest[kStreamWarps];
     float listed_logit[kMaxTopLogits];                     // the slice's listed entries' own logits
     int bad, twice;
 };
@@ -52,48 +52,61 @@ struct Slice : RowSlice<T, kStreamers> {
 __device__ __forceinline__ uint32_t unit_bits(int i) { return reinterpret_cast<const uint8_t*>(listed_bits)[i]; }
 
 // ---- the list's warp ----------------------------------------------------------------------------
-// Marks the slice's listed ids; notes whether an id is listed twice, or lies outside the vocabulary.
+// Marks the slice's listed ids; notes whether an id is listed twice, or lies outside the vocabulary.  Returns which of the lane's
+// entries (a bit each) are the first of their id.
 template <typename T>
-__device__ void mark_listed(const DistillArgs& a, int64_t r, const Slice<T>& slice, Shared& s) {
-    for (int j = threadIdx.x & 31; j < a.K; j += 32) {
+__device__ uint32_t mark_listed(const DistillArgs& a, int64_t r, const Slice<T>& slice, Shared& s) {
+    uint32_t first = 0, mine = 1;
+    for (int j = threadIdx.x & 31; j < a.K; j += 32, mine <<= 1) {
         const int id = a.top_ids[r * a.K + j];
         if (id >= a.V) s.bad = 1;
         const int i = slice.index_of(id);
         if (i < 0) continue;
         const uint32_t bit = 1u << ((i & 3) * 8 + (id + slice.row.lead) % Elem<T>::kWidth);
         if (atomicOr(&listed_bits[i >> 2], bit) & bit) s.twice = 1;
+        else first |= mine;
     }
+    return first;
 }
+static_assert(kMaxTopLogits <= 32 * 32, "a bit for each of a lane's entries");
 
-// The sums over every `shares`-th entry of the list, from `share` on; with `logits` the cross sums as well.
+// The teacher's sums: with `student` over the slice's entries, with their part in the student's and the cross sums; else over all.
 template <typename T>
-__device__ void list_sums(const DistillArgs& a, int64_t r, const T* row, int shares, int share, bool logits, Part& part) {
-    const int first = (threadIdx.x & 31) * shares + share, step = 32 * shares;
+__device__ void list_sums(const DistillArgs& a, int64_t r, const Slice<T>& slice, bool student, uint32_t firsts, float c, Shared& s,
+                          Part& part) {
     const int32_t* ids = a.top_ids + r * a.K;
     const float* t = a.top_values + r * a.K;
+    auto missing = [&](int id) { return student ? slice.index_of(id) < 0 : id < 0 || id >= a.V; };
     float most = -INFINITY, near = -INFINITY;
-    for (int j = first; j < a.K; j += step)
-        if (ids[j] >= 0 && ids[j] < a.V) {
-            most = fmaxf(most, t[j]);
-            if (logits) near = fmaxf(near, Elem<T>::to_float(row[ids[j]]));
-        }
+    for (int j = threadIdx.x & 31; j < a.K; j += 32) {
+        const int id = ids[j];
+        if (missing(id)) continue;
+        most = fmaxf(most, t[j]);
+        if (!student) continue;
+        const float logit = Elem<T>::to_float(slice.row.row[id]);
+        s.listed_logit[j] = logit;
+        near = fmaxf(near, logit);
+    }
     most = warp_reduce(most, MaxOp());
-    near = logits ? warp_reduce(near, MaxOp()) : 0.0f;
-    part.near = near == -INFINITY ? 0.0f : near;
+    part.near = student ? warp_reduce(near, MaxOp()) : -INFINITY;
     part.ref = a.top_lse ? (double)a.top_lse[r] : (double)most * (double)a.inv_t;
     part.mass = part.cross = 0.0;
     part.lost = -INFINITY;
-    for (int j = first; j < a.K; j += step) {
-        const int id = ids[j];
-        if (id < 0 || id >= a.V || t[j] == -INFINITY) continue;
+    part.listed = 0.0f;
+    const float from = finite_or_zero(part.near);
+    for (int j = threadIdx.x & 31; j < a.K; j += 32, firsts >>= 1) {
+        if (missing(ids[j])) continue;
+        if (student && a.top_lse && (firsts & 1u)) part.listed += fast_exp2((s.listed_logit[j] - from) * c);
+        if (t[j] == -INFINITY) continue;
         const double x = (double)t[j] * (double)a.inv_t - part.ref, e = exp(x);
         part.mass += e;
-        if (!logits || e == 0.0) continue;
-        const float logit = Elem<T>::to_float(row[id]);
+        if (!student || e == 0.0) continue;
+        const float logit = s.listed_logit[j];
         if (logit == -INFINITY) part.lost = fmaxf(part.lost, t[j]);
-        else part.cross += e * (x - ((double)logit - (double)part.near) * (double)a.inv_t);
+        else part.cross += e * (x - ((double)logit - (double)from) * (double)a.inv_t);
     }
     part.lost = warp_reduce(part.lost, MaxOp());
+    part.listed = warp_reduce(part.listed, AddOp());
     part.mass = warp_reduce(part.mass, AddOp());
     part.cross = warp_reduce(part.cross, AddOp());
 }
@@ -112,7 +125,7 @@ __device__ __forceinline__ void read_slice(const Slice<T>& slice, uint4* q, floa
     RunningSums<T> sums(c);
     const int step = slice.step;
     int u = slice.start(threadIdx.x), i = threadIdx.x;
-    auto add = [&](auto count, const uint4* units) {       // units whose bits stand kStreamers apart
+    auto add = [&](auto count, uint4* units) {       // units whose bits stand kStreamers apart
         constexpr int kUnits = decltype(count)::value;
         uint32_t bits[kUnits];
 #pragma unroll
@@ -148,9 +161,7 @@ __device__ __forceinline__ void block_sums(const Shared& s, float c, Part& part)
     const int lane = threadIdx.x & 31;
     const float top = lane < kStreamWarps ? s.top[lane] : -INFINITY;
     part.top = warp_reduce(top, MaxOp());
-    const float f = top == -INFINITY || top == part.top ? 1.0f : fast_exp2((top - part.top) * c);
-    part.all = (float)warp_reduce(lane < kStreamWarps ? (double)s.all[lane] * f : 0.0, AddOp());
-    part.rest = (float)warp_reduce(lane < kStreamWarps ? (double)s.rest[lane] * f : 0.0, AddOp());
+    part.rest = (float)warp_reduce(lane < kStreamWarps ? (double)s.rest[lane] * moved(top, part.top, c) : 0.0, AddOp());
 }
 
 // The slice as if nothing were listed; the first batch is there already if it is wanted at all.
@@ -164,7 +175,7 @@ __device__ __forceinline__ void write_unlisted(const Slice<T>& slice, uint4* q, 
             for (int e = 0; e < Elem<T>::kWidth; ++e) {
                 const int v = slice.row.first(u) + e;
                 if (v >= 0 && v < slice.row.V)
-                    grad[v] = Elem<T>::from_float(g.rest * g.ex.of_logit(Elem<T>::to_float(slice.row.row[v])));
+                    grad[v] = Elem<T>::from_float(g.unlisted(Elem<T>::to_float(slice.row.row[v])));
             }
         return;
     }
@@ -206,19 +217,17 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_rows_kernel(const
     }
     const float weight = a.row_weight ? a.row_weight[r] : 1.0f;
     __syncthreads();
-    if (lists && weight != 0.0f) mark_listed(a, r, slice, s);
+    uint32_t firsts = 0;
+    if (lists && weight != 0.0f) firsts = mark_listed(a, r, slice, s);
     __syncthreads();
     const bool bad = s.bad != 0, skip = weight == 0.0f || bad;        // the same in all CTAs of the row
 
     Part part = no_part();
     if (!skip) {
         if (lists) {
-            if (kMode != kBackward) {
-                list_sums(a, r, slice.row.row, ranks, rank, true, part);
-            } else {                                       // the whole list: there is no exchange
-                list_sums(a, r, slice.row.row, 1, 0, false, part);
-            }
-            if (kMode != kForward)                         // before anything is written: the gradient may replace the logits
+            // (backward: the whole list, there is no exchange)
+            list_sums(a, r, slice, kMode != kBackward, firsts, c, s, part);
+            if (kMode == kBackward)                        // before anything is written: the gradient may replace the logits
                 for (int j = threadIdx.x & 31; j < a.K; j += 32) {
                     const int id = a.top_ids[r * a.K + j];
                     if (slice.index_of(id) >= 0) s.listed_logit[j] = Elem<T>::to_float(slice.row.row[id]);
@@ -228,7 +237,6 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_rows_kernel(const
             if ((threadIdx.x & 31) == 0) {
                 const int w = threadIdx.x >> 5;
                 s.top[w] = part.top;
-                s.all[w] = part.all;
                 s.rest[w] = part.rest;
             }
         }
@@ -260,13 +268,13 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_rows_kernel(const
     const Part mine = lane < (kMode == kBackward ? 1 : ranks) ? s.part[lane] : no_part();
     Row row;
     combine_teacher(a, mine, row);
-    if (kMode != kBackward) combine_student(a, mine, c, row);
-    if (kMode == kBackward) { row.top = a.stats[3 * r]; row.sum = a.stats[3 * r + 1]; row.rest = a.stats[3 * r + 2]; }
+    if (kMode != kBackward) combine_student(a, mine, combine_listed(mine, c), c, row);
+    if (kMode == kBackward) student_from_stats(a, r, row);
     if (kMode != kBackward && lists && rank == 0) {
         const float loss = row_loss(a, mine, row);
         if (threadIdx.x == kStreamers) {
             a.loss[r] = weight * loss;
-            if (kMode == kForward && a.stats) { a.stats[3 * r] = row.top; a.stats[3 * r + 1] = row.sum; a.stats[3 * r + 2] = row.rest; }
+            if (kMode == kForward && a.stats) { a.stats[3 * r] = row.top; a.stats[3 * r + 1] = row.sum; a.stats[3 * r + 2] = rest_to_stats(a, row); }
         }
     }
     if (kMode == kForward) return;
@@ -284,8 +292,7 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_rows_kernel(const
         } else {
             q_id = teacher_q(a.top_values[r * a.K + j], a.inv_t, row.norm);
         }
-        const float p = g.ex.of_logit(s.listed_logit[j]) * g.inv_sum;
-        grad[id] = Elem<T>::from_float(g.scale * (p * g.S - q_id));
+        grad[id] = Elem<T>::from_float(g.listed(s.listed_logit[j], q_id));
     }
 }
 

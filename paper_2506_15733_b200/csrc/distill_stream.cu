@@ -39,7 +39,7 @@ struct Slot {
     int edge_id[16];                                       // -1: none
     double edge_q[16];                                     // what the list gives them, < 0: not listed
     uint32_t flags[kTakeWarps][kFlagWords];                // which of a warp's units, 32 at a time, have listed entries
-    float top[kTakeWarps], all[kTakeWarps], rest[kTakeWarps];
+    float top[kTakeWarps], rest[kTakeWarps], listed[kListWarps];    // sums of the taking warps, and of the list warps' entries
     int skip, bad;
 };
 struct StreamShared {
@@ -96,9 +96,10 @@ __device__ __forceinline__ bool take_row(StreamShared& s, const Slot& slot, cons
 
 template <typename T>
 __device__ bool take_sums(StreamShared& s, const Slot& slot, const uint32_t* head, const uint8_t* stages, int stage_count,
-                          RingPlace& at, const StreamRow<T>& row, float c, const BoundedWait& wait, Part& part) {
+                          RingPlace& at, const StreamRow<T>& row, float c, const BoundedWait& wait, bool lists, Part& part) {
     RunningSums<T> sums(c);
-    const bool fine = take_row(s, slot, stages, stage_count, at, row, wait, [&](const uint4* q, int k, uint32_t flag) {
+    const bool fine = take_row(s, slot, stages, stage_count, at, row, wait, [&](uint4* q, int k, uint32_t flag) {
+        if (!lists) flag = 0;
         sums.template add<kTake>(q, [&](int j) { return ((flag >> j) & 1u) != 0; }, [&](int j) {
             uint32_t bits = 0;
             walk_group<T>(slot, head, (k + j * kTakers) >> 5, [&](int, int e) { bits |= 1u << e; });
@@ -135,8 +136,7 @@ __device__ bool take_gradient(StreamShared& s, const Slot& slot, const uint32_t*
             }
             if ((flag >> j) & 1u)                          // over what the same thread has just written
                 walk_group<T>(slot, head, u >> 5, [&](int entry, int e) {
-                    const float p = g.ex.of_logit(unit_element<T>(q[j], e)) * g.inv_sum;
-                    to[e] = Elem<T>::from_float(zero ? 0.0f : g.scale * (p * g.S - slot.q[entry]));
+                    to[e] = Elem<T>::from_float(zero ? 0.0f : g.listed(unit_element<T>(q[j], e), slot.q[entry]));
                 });
         }
     });
@@ -199,7 +199,8 @@ __device__ void load_list(const DistillArgs& a, int64_t r, Slot& slot, uint32_t*
     Part part = no_part();
     most = warp_reduce(most, MaxOp());
     near = warp_reduce(near, MaxOp());
-    part.near = near == -INFINITY ? 0.0f : near;
+    part.near = near;
+    near = finite_or_zero(near);
     part.ref = a.top_lse ? (double)a.top_lse[r] : (double)most * (double)a.inv_t;
     part.mass = part.cross = 0.0;
 #pragma unroll
@@ -209,17 +210,31 @@ __device__ void load_list(const DistillArgs& a, int64_t r, Slot& slot, uint32_t*
         part.mass += e;
         if (kMode == kBackward || e == 0.0) continue;
         if (logit[i] == -INFINITY) part.lost = fmaxf(part.lost, value[i]);
-        else part.cross += e * (x - ((double)logit[i] - (double)part.near) * (double)a.inv_t);
+        else part.cross += e * (x - ((double)logit[i] - (double)near) * (double)a.inv_t);
     }
     part.lost = warp_reduce(part.lost, MaxOp());
     part.mass = warp_reduce(part.mass, AddOp());
     part.cross = warp_reduce(part.cross, AddOp());
     if (lane == 0) slot.part[warp] = part;
     listers_meet();
+    if (kMode != kBackward && a.top_lse) {                 // the student's sum over the listed ids, each of them once
+        float listed = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int j = t + i * kListers;
+            if (j >= a.K || slot.pos[j] < 0) continue;
+            bool first = true;
+            for (uint32_t entry = head[slot.pos[j] / Elem<T>::kWidth >> 5]; entry; entry = slot.next[entry - 1])
+                first &= slot.pos[entry - 1] != slot.pos[j] || (int)entry - 1 >= j;
+            if (first) listed += fast_exp2((logit[i] - near) * (a.inv_t * kLog2e));
+        }
+        listed = warp_reduce(listed, AddOp());
+        if (lane == 0) slot.listed[warp] = listed;
+    }
     Row known;
     combine_teacher(a, lane < kListWarps ? slot.part[lane] : no_part(), known);
     if (t == 0) {
-        if (kMode == kBackward) { known.top = a.stats[3 * r]; known.sum = a.stats[3 * r + 1]; known.rest = a.stats[3 * r + 2]; }
+        if (kMode == kBackward) student_from_stats(a, r, known);
         slot.row = known;
     }
 #pragma unroll
@@ -256,26 +271,33 @@ __device__ void load_list(const DistillArgs& a, int64_t r, Slot& slot, uint32_t*
     }
 }
 
-// The finishing warp: the row's sums, which the gradient pass waits for; its loss; the partial units' gradient.
+// The finishing warp: the row's sums, which the gradient pass waits for; its loss; the partial units' gradient.  What the list
+// alone gives is worked out while the taking warps are still at it.  False when a wait ran out.
 template <typename T, int kMode>
-__device__ void finish_row(const DistillArgs& a, int64_t r, Slot& slot, uint64_t* row_full, float c) {
+__device__ bool finish_row(const DistillArgs& a, int64_t r, Slot& slot, const SlotPlace& place, StreamShared& s, float c,
+                           const BoundedWait& wait) {
     const int lane = threadIdx.x & 31;
     const int edge = lane >= 16 ? slot.edge_id[lane - 16] : -1;
     const float logit = edge >= 0 ? slot.edge[lane - 16] : -INFINITY;
     const double edge_q = edge >= 0 ? slot.edge_q[lane - 16] : -1.0;
     const bool bad = slot.bad != 0;
     Row row = slot.row;
+    Part p = no_part();
+    Listed listed = {-INFINITY, 0.0f};
     if (kMode != kBackward) {
-        Part p = no_part();
-        if (lane < kTakeWarps) { p.top = slot.top[lane]; p.all = slot.all[lane]; p.rest = slot.rest[lane]; }
+        if (lane < kListWarps && a.top_lse) { p.near = slot.part[lane].near; p.listed = slot.listed[lane]; }
         if (edge >= 0) {                                   // an entry by itself: its sum is 1 (NaN for NaN and inf, 0 for -inf)
-            p.top = fmaxf(logit, -INFINITY);
-            p.all = logit == -INFINITY ? 0.0f : 1.0f + (logit - logit);
-            p.rest = edge_q >= 0.0 ? 0.0f : p.all;
+            const float most = fmaxf(logit, -INFINITY), sum = logit == -INFINITY ? 0.0f : 1.0f + (logit - logit);
+            if (a.top_lse && edge_q >= 0.0) { p.near = most; p.listed = sum; } else { p.top = most; p.rest = sum; }
         }
-        combine_student(a, p, c, row);
+        listed = combine_listed(p, c);
+    }
+    if (!__all_sync(kAllLanes, wait(&s.sums_full[place.slot], place.phase))) return false;
+    if (kMode != kBackward) {
+        if (lane < kTakeWarps) { p.top = slot.top[lane]; p.rest = slot.rest[lane]; }
+        combine_student(a, p, listed, c, row);
         if (kMode == kStep) {
-            if (lane == 0) { slot.row = row; barrier_arrive(row_full); }
+            if (lane == 0) { slot.row = row; barrier_arrive(&s.row_full[place.slot]); }
             __syncwarp();
         }
         const float loss = row_loss(a, lane < kListWarps ? slot.part[lane] : no_part(), row);
@@ -284,18 +306,18 @@ __device__ void finish_row(const DistillArgs& a, int64_t r, Slot& slot, uint64_t
             if (kMode == kForward && a.stats) {
                 a.stats[3 * r] = bad ? 0.0f : row.top;
                 a.stats[3 * r + 1] = bad ? 0.0f : row.sum;
-                a.stats[3 * r + 2] = bad ? 0.0f : row.rest;
+                a.stats[3 * r + 2] = bad ? 0.0f : rest_to_stats(a, row);
             }
         }
     }
     if (lane == 0 && bad) atomicOr(a.status, SPECS_DEV_TOKEN_RANGE);
     if (kMode != kForward && edge >= 0) {
         const Gradient g(row, c, slot.scale);
-        const float p = g.ex.of_logit(logit);
-        float v = edge_q >= 0.0 ? g.scale * (p * g.inv_sum * g.S - (float)edge_q) : g.rest * p;
+        float v = edge_q >= 0.0 ? g.listed(logit, (float)edge_q) : g.unlisted(logit);
         if (bad) v = 0.0f;
         (static_cast<T*>(a.grad) + r * a.grad_stride)[edge] = Elem<T>::from_float(v);
     }
+    return true;
 }
 
 template <typename T, int kMode>
@@ -359,10 +381,9 @@ distill_stream_kernel(const DistillArgs a, int stage_count, int groups) {
                 }
             } else if (kMode != kBackward) {
                 Part part;
-                if (!take_sums(s, slot, head, stages, stage_count, at, row, c, wait, part)) return;
+                if (!take_sums(s, slot, head, stages, stage_count, at, row, c, wait, a.top_lse != nullptr, part)) return;
                 if (lane == 0) {
                     slot.top[warp] = part.top;
-                    slot.all[warp] = part.all;
                     slot.rest[warp] = part.rest;
                 }
             }
@@ -381,10 +402,11 @@ distill_stream_kernel(const DistillArgs a, int stage_count, int groups) {
         SlotPlace place;
         for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, place.next()) {
             Slot& slot = s.slot[place.slot];
-            if (!__all_sync(kAllLanes, wait(&s.sums_full[place.slot], place.phase))) return;
+            if (!__all_sync(kAllLanes, wait(&s.list_full[place.slot], place.phase))) return;
             if (!slot.skip) {
-                finish_row<T, kMode>(a, r, slot, &s.row_full[place.slot], c);
+                if (!finish_row<T, kMode>(a, r, slot, place, s, c, wait)) return;
             } else {
+                if (!__all_sync(kAllLanes, wait(&s.sums_full[place.slot], place.phase))) return;
                 if (lane == 0 && kMode == kStep) barrier_arrive(&s.row_full[place.slot]);
                 if (lane == 0 && kMode != kBackward) a.loss[r] = 0.0f;
                 if (lane < 3 && kMode == kForward && a.stats) a.stats[3 * r + lane] = 0.0f;
