@@ -479,7 +479,7 @@ int specs_top_logits(specs_ctx* ctx, const void* logits, int dtype, int64_t row_
  *                        from fp32.  May be `logits` itself (with the same stride), never another overlap.
  * specs_distill_step is forward and backward in one pass over the logits, for a training step whose
  * grad_loss is known beforehand.  A student's logit of -inf has p = 0: the loss is +inf where the
- * teacher gives it any mass.  NaN logits give a NaN loss and gradient. */
+ * teacher gives it any mass.  NaN logits give a NaN loss and gradient, also where all the mass is the remaining one. */
 int specs_distill_forward(specs_ctx* ctx, const void* logits, int dtype, int64_t row_stride, int64_t rows, int32_t V,
                           const int32_t* top_ids, const float* top_values, const float* top_lse, int32_t K,
                           float temperature, const float* row_weight, float* loss, float* stats, void* cuda_stream);

@@ -117,8 +117,8 @@ def distill(logits, top_ids, top_values, temperature=1.0, top_lse=None, row_weig
             listed = np.zeros(V, dtype=bool)
             listed[[i for i, _ in here]] = True
             total, rest = e.sum(), e[~listed].sum()
-            q_r = max(0.0, 1.0 - q.sum()) if top_lse is not None and rest > 0 else 0.0
-            if q_r > 0 and (top - float(np.nanmax(x[~listed]))) / T > 690:   # what lies further down counts as nothing
+            q_r = max(0.0, 1.0 - q.sum()) if top_lse is not None and not rest == 0 else 0.0
+            if q_r > 0 and not np.isnan(rest) and (top - float(np.nanmax(x[~listed]))) / T > 690:   # what lies further down counts as nothing
                 q_r = 0.0
             S = q.sum() + q_r
             value = 0.0

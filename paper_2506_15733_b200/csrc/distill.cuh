@@ -82,14 +82,17 @@ __device__ __forceinline__ void combine_student(const DistillArgs& a, const Part
     row.top = fmaxf(row.rest_top, listed.near);            // (without top_lse all of these are in rest_top, and listed.sum is 0)
     row.rest = row.rest_own * moved(row.rest_top, row.top, c);
     row.sum = row.rest + listed.sum * moved(listed.near, row.top, c);
-    if (!(row.rest_own > 0.0f) || ((double)row.top - (double)row.rest_top) * (double)a.inv_t > kLeastRest) row.left = 0.0f;
+    const bool none = row.rest_own == 0.0f || ((double)row.top - (double)row.rest_top) * (double)a.inv_t > kLeastRest;
+    if (none && row.rest_own == row.rest_own) row.left = 0.0f;         // (NaN stays one)
 }
 
 // What the forward pass leaves of the unlisted part for the backward pass: itself, or its logarithm where it is below the normal
 // floats (which is negative, while it is not); 0 where it does not count.
 __device__ __forceinline__ float rest_to_stats(const DistillArgs& a, const Row& row) {
     const double down = ((double)row.rest_top - (double)row.top) * (double)a.inv_t;
-    if (!a.top_lse || row.rest_own == 0.0f || down < -kLeastRest) return 0.0f;
+    if (!a.top_lse || row.rest_own == 0.0f) return 0.0f;
+    if (row.rest_own != row.rest_own) return row.rest_own;
+    if (down < -kLeastRest) return 0.0f;
     const double rest = (double)row.rest_own * exp(down);
     return rest < 1.1754943508222875e-38 ? (float)(log((double)row.rest_own) + down) : (float)rest;
 }
@@ -97,8 +100,8 @@ __device__ __forceinline__ void student_from_stats(const DistillArgs& a, int64_t
     row.top = row.rest_top = a.stats[3 * r];
     row.sum = a.stats[3 * r + 1];
     const float rest = a.stats[3 * r + 2];
-    row.rest = row.rest_own = fmaxf(rest, 0.0f);
-    if (!(rest != 0.0f) || rest != rest) {
+    row.rest = row.rest_own = rest < 0.0f ? 0.0f : rest;
+    if (rest == 0.0f) {
         row.left = 0.0f;
     } else if (rest < kNearRest) {                         // relative to a logit about as large as the largest unlisted one
         const double ln_rest = rest < 0.0f ? (double)rest : log((double)rest);
