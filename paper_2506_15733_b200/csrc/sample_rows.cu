@@ -34,7 +34,7 @@ constexpr int kMassBins = 1024, kCoarse = 64, kFine = kMassBins / kCoarse;
 constexpr float kBinsPerUnit = 45.0f;        // bins per unit of the exponent: weights end at 22.2, bin 999
 constexpr int kBins = 64, kMaxLevels = 12;   // narrowing: 32 bits of a key and 19 of an id, 6 a level, take 10 at most
 constexpr int kTargetCtas = 296, kLeastUnits = 1024, kLongUnits = 16384;
-constexpr uint32_t kHighestKey = 0xffffffffu;
+constexpr uint32_t kHighestKey = 0xffffffffu, kKeyOfMinusZero = 0x7fffffffu;   // order_key has both zeros at 0x80000000
 
 // Temperature in the exponent.  NaN and what is too small to weigh anything become -30, so that no special case remains.
 __device__ __forceinline__ float scaled(float l, float top, float inv_t) { return fmaxf((l - top) * inv_t, -30.0f); }
@@ -289,7 +289,8 @@ __device__ __forceinline__ void push_entry(Shared& s, Shared* home, uint32_t key
 template <typename T>
 __device__ __forceinline__ void push_unit(Shared& s, Shared* home, const uint4& q, int id, uint32_t lo, uint32_t hi, int first,
                                           int last) {
-    const float least = key_value(lo), most = hi == kHighestKey ? INFINITY : key_value(hi);
+    // (as numbers; an interval that ends at the key of -0, which no entry has, ends at the number below the zeros)
+    const float least = key_value(lo), most = hi == kHighestKey ? INFINITY : key_value(hi == kKeyOfMinusZero ? hi - 1 : hi);
     float f[Elem<T>::kWidth];
     uint32_t in = 0;
     Elem<T>::widen(q, f);
@@ -783,9 +784,8 @@ __global__ void __launch_bounds__(kThreads, 2) top_rows_kernel(const TopArgs a) 
             search<T>(c, slice, st, false, (uint64_t)a.K - 1, row.top, a.inv_t, 1);
             const uint32_t key = place_key(s.found_place);
             const int id = place_id(s.found_place);
-            push_entries(c, slice, st, key + 1, kHighestKey, 0, a.V - 1, 0);
-            push_entries(c, slice, st, key, key, 0, id, 1);
-            n = a.K;
+            n = (int)push_entries(c, slice, st, key + 1, kHighestKey, 0, a.V - 1, 0);
+            n = min(kListCap, n + (int)push_entries(c, slice, st, key, key, 0, id, 1));
         }
     }
     if (c.rank != 0) return;
