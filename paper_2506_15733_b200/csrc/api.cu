@@ -130,7 +130,7 @@ int specs_create(specs_ctx** out, int device) {
         return SPECS_ERR_CUDA;
     }
     ctx->pair_units = query_pair_units(device, ctx->num_sms);
-    if (!prepare_pick_rows()) {
+    if (!prepare_pick_rows() || !prepare_top_stream() || !prepare_distill_rows() || !prepare_distill_stream()) {
         cudaFree(ctx->d_status);
         delete ctx;
         return SPECS_ERR_CUDA;

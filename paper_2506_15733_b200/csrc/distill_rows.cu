@@ -315,10 +315,17 @@ int launch_typed(const DistillArgs& a, cudaStream_t stream) {
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cfg.dynamicSmemBytes > 40960 && cudaFuncSetAttribute(distill_rows_kernel<T, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                             (int)cfg.dynamicSmemBytes) != cudaSuccess)
-        return SPECS_ERR_CUDA;
     return cuda_status(cudaLaunchKernelEx(&cfg, distill_rows_kernel<T, kMode>, a, shift));
+}
+
+template <typename T>
+bool prepare_typed() {
+    constexpr int kMost = padded_units((kMaxRowVocab / Elem<T>::kWidth + 2 + 31) / 32 * 32);      // a whole row of the longest
+    const void* kernels[] = {(const void*)distill_rows_kernel<T, kForward>, (const void*)distill_rows_kernel<T, kBackward>,
+                             (const void*)distill_rows_kernel<T, kStep>};
+    for (const void* k : kernels)
+        if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost) != cudaSuccess) return false;
+    return true;
 }
 
 // One persistent CTA per SM (distill_stream.cu) for more rows than SMs that are long enough for its lists to be fetched behind
@@ -338,6 +345,8 @@ int launch(const DistillArgs& a, int dtype, cudaStream_t stream) {
 }
 
 }  // namespace
+
+bool prepare_distill_rows() { return prepare_typed<float>() && prepare_typed<__nv_bfloat16>() && prepare_typed<__half>(); }
 
 int launch_distill_forward(const DistillArgs& a, int dtype, cudaStream_t stream) { return launch<kForward>(a, dtype, stream); }
 int launch_distill_backward(const DistillArgs& a, int dtype, cudaStream_t stream) { return launch<kBackward>(a, dtype, stream); }

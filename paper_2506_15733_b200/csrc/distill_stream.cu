@@ -438,11 +438,18 @@ int launch_stream(const DistillArgs& a, cudaStream_t stream) {
     const int fixed = (int)sizeof(StreamShared) + kSlots * groups * 4;
     const int room = (kSharedPerBlock - fixed) / kStageBytes, stages = room < kRingStages ? room : kRingStages;
     const int bytes = stages * kStageBytes + fixed;
-    if (cudaFuncSetAttribute(distill_stream_kernel<T, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess)
-        return SPECS_ERR_CUDA;
     const int grid = a.rows < a.num_sms ? (int)a.rows : a.num_sms;
     distill_stream_kernel<T, kMode><<<grid, kStreamBlock, bytes, stream>>>(a, stages, groups);
     return cuda_status(cudaGetLastError());
+}
+
+template <typename T>
+bool prepare_typed() {
+    const void* kernels[] = {(const void*)distill_stream_kernel<T, kForward>, (const void*)distill_stream_kernel<T, kBackward>,
+                             (const void*)distill_stream_kernel<T, kStep>};
+    for (const void* k : kernels)
+        if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedPerBlock) != cudaSuccess) return false;
+    return true;
 }
 
 template <int kMode>
@@ -455,6 +462,8 @@ int launch_mode(const DistillArgs& a, int dtype, cudaStream_t stream) {
 }
 
 }  // namespace
+
+bool prepare_distill_stream() { return prepare_typed<float>() && prepare_typed<__nv_bfloat16>() && prepare_typed<__half>(); }
 
 int launch_distill_stream(const DistillArgs& a, int dtype, int mode, cudaStream_t stream) {
     return mode == kForward ? launch_mode<kForward>(a, dtype, stream)

@@ -336,8 +336,12 @@ struct DistillArgs {
     float* loss; float* stats; void* grad; int64_t grad_stride;
     uint32_t* status; int num_sms;
 };
-// Opts the kernels in to their shared memory on the current device (once per context).
+// Opt the kernels in to the most shared memory that any call needs, on the current device.  Once per context and not per launch:
+// the limit belongs to the function, and a launch in another host thread may need more than the one that sets it.
 bool prepare_pick_rows();
+bool prepare_top_stream();
+bool prepare_distill_rows();
+bool prepare_distill_stream();
 int launch_sample_rows(const SampleArgs& a, int dtype, cudaStream_t stream);
 int launch_top_rows(const TopArgs& a, int dtype, cudaStream_t stream);
 int launch_top_stream(const TopArgs& a, int dtype, cudaStream_t stream);    // top_stream.cu: K <= kStreamTop

@@ -429,14 +429,20 @@ template <typename T>
 int launch_stream(const TopArgs& a, cudaStream_t stream) {
     const int room = (kSharedPerBlock - (int)sizeof(StreamShared)) / kStageBytes, stages = room < kRingMax ? room : kRingMax;
     const int bytes = stages * kStageBytes + (int)sizeof(StreamShared);
-    if (cudaFuncSetAttribute(top_stream_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess)
-        return SPECS_ERR_CUDA;
     const int grid = a.rows < a.num_sms ? (int)a.rows : a.num_sms;
     top_stream_kernel<T><<<grid, kStreamBlock, bytes, stream>>>(a, stages);
     return cuda_status(cudaGetLastError());
 }
 
 }  // namespace
+
+bool prepare_top_stream() {
+    const void* kernels[] = {(const void*)top_stream_kernel<float>, (const void*)top_stream_kernel<__nv_bfloat16>,
+                             (const void*)top_stream_kernel<__half>};
+    for (const void* k : kernels)
+        if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedPerBlock) != cudaSuccess) return false;
+    return true;
+}
 
 int launch_top_stream(const TopArgs& a, int dtype, cudaStream_t stream) {
     return dtype == SPECS_F32 ? launch_stream<float>(a, stream)
