@@ -221,6 +221,14 @@ def _list_length(t, name: str) -> int:
     return t.shape[1]
 
 
+def _pitched(t, per_row: int, name: str):
+    """``t``, unless it has rows of another length than ``per_row``, which would be read as somebody else's numbers.  A flat
+    tensor has none."""
+    if hasattr(t, "dim") and t.dim() != 1 and (t.dim() != 2 or t.shape[1] != per_row):
+        raise ValueError(f"{name}: expected [rows, {per_row}], got {list(t.shape)}")
+    return t
+
+
 def score_plan(rows: int, d: int, V: int, num_sms: int, cta_group: int = 0) -> dict:
     out = (_i32 * 16)()
     _check(load_library().specs_score_plan(rows, d, V, num_sms, cta_group, out), "specs_score_plan")
@@ -491,7 +499,8 @@ class Context:
         K = _list_length(top_ids, "top_ids")
         _check(self._lib.specs_top_logits(
             self._h, ptr, code, stride, rows, V, K, float(temperature), a(top_ids, "i32", rows * K, "top_ids"),
-            a(top_values, "f32", rows * K, "top_values"), a(lse, "f32", rows, "lse"), self._s()), "specs_top_logits")
+            a(_pitched(top_values, K, "top_values"), "f32", rows * K, "top_values"), a(lse, "f32", rows, "lse"), self._s()),
+            "specs_top_logits")
 
     def _distill(self, logits, top_ids, top_values, top_lse, temperature):
         """The leading arguments of the three distillation calls, and the number of rows."""
@@ -499,8 +508,8 @@ class Context:
         ptr, code, stride, rows, V = rows_arg(logits, self.device, "logits")
         K = _list_length(top_ids, "top_ids")
         return (self._h, ptr, code, stride, rows, V, a(top_ids, "i32", rows * K, "top_ids"),
-                a(top_values, "f32", rows * K, "top_values"), a(top_lse, "f32", rows, "top_lse"), K,
-                float(temperature)), rows
+                a(_pitched(top_values, K, "top_values"), "f32", rows * K, "top_values"),
+                a(top_lse, "f32", rows, "top_lse"), K, float(temperature)), rows
 
     def _grad(self, logits, grad_logits):
         ptr, _, stride, rows, V = rows_arg(grad_logits, self.device, "grad_logits")
@@ -517,7 +526,8 @@ class Context:
         head, rows = self._distill(logits, top_ids, top_values, top_lse, temperature)
         a = self._a
         _check(self._lib.specs_distill_forward(*head, a(row_weight, "f32", rows, "row_weight"), a(loss, "f32", rows, "loss"),
-                                               a(stats, "f32", 3 * rows, "stats"), self._s()), "specs_distill_forward")
+                                               a(_pitched(stats, 3, "stats"), "f32", 3 * rows, "stats"), self._s()),
+               "specs_distill_forward")
 
     def specs_distill_backward(self, logits, top_ids, top_values, stats, grad_logits, temperature=1.0, top_lse=None,
                                row_weight=None, grad_loss=None):
@@ -527,8 +537,9 @@ class Context:
         grad, stride = self._grad(logits, grad_logits)
         a = self._a
         _check(self._lib.specs_distill_backward(*head, a(row_weight, "f32", rows, "row_weight"),
-                                                a(stats, "f32", 3 * rows, "stats"), a(grad_loss, "f32", rows, "grad_loss"),
-                                                grad, stride, self._s()), "specs_distill_backward")
+                                                a(_pitched(stats, 3, "stats"), "f32", 3 * rows, "stats"),
+                                                a(grad_loss, "f32", rows, "grad_loss"), grad, stride, self._s()),
+               "specs_distill_backward")
 
     def specs_distill_step(self, logits, top_ids, top_values, loss, grad_logits, temperature=1.0, top_lse=None,
                            row_weight=None, grad_loss=None):
