@@ -451,11 +451,12 @@ int specs_sample_tokens(specs_ctx* ctx, const void* logits, int dtype, int64_t r
  *   top_ids    int32 [rows, K] out, top_values float [rows, K] out: the ids and the logits themselves (not
  *              divided by T); a row with fewer than K logits above -inf is filled up with -1 and -inf.
  *   lse        float [rows] out or NULL: ln sum_v exp(l_v / T) over all V entries, NaN where a logit is NaN
- *              or +inf, -inf for a row without any logit above -inf.  T = temperature > 0. */
+ *              or +inf, -inf for a row without any logit above -inf.  T = temperature > 0, and
+ *              large enough that log2(e) / T is a float, from about 4.3e-39 on (SPECS_ERR_SHAPE otherwise). */
 int specs_top_logits(specs_ctx* ctx, const void* logits, int dtype, int64_t row_stride, int64_t rows, int32_t V,
                      int32_t K, float temperature, int32_t* top_ids, float* top_values, float* lse, void* cuda_stream);
 
-/* Distillation of a student from a teacher's top logits, at temperature T > 0.  Per row, with the student's
+/* Distillation of a student from a teacher's top logits, at a temperature T as in specs_top_logits.  Per row, with the student's
  * p = softmax(logits / T) over all V and the teacher's list of K entries (id_j, t_j):
  *   q_j  = exp(t_j / T - top_lse)             with top_lse float [rows], the teacher's own ln sum exp(. / T) as
  *                                             specs_top_logits gives it at the same T

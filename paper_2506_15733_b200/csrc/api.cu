@@ -624,6 +624,9 @@ static int check_rows(const void* logits, int dtype, int64_t row_stride, int64_t
     return (reinterpret_cast<uintptr_t>(logits) & (dtype == SPECS_F32 ? 3u : 1u)) == 0 ? SPECS_OK : SPECS_ERR_ALIGN;
 }
 
+// The kernels take exponentials as powers of two, by log2(e) / T: that has to be a float above 0.
+static bool good_temperature(float t) { return t > 0.0f && t <= FLT_MAX && 1.0f / t * 1.44269504f <= FLT_MAX; }
+
 int specs_sample_tokens(specs_ctx* ctx, const void* logits, int dtype, int64_t row_stride, int64_t rows, int32_t V,
                         const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                         const float* uniforms, int32_t* tokens, float* tok_logprob, float* draw_logprob,
@@ -644,7 +647,7 @@ int specs_top_logits(specs_ctx* ctx, const void* logits, int dtype, int64_t row_
     if (!ctx) return SPECS_ERR_NULL;
     const int st = check_rows(logits, dtype, row_stride, rows, V);
     if (st != SPECS_OK) return st;
-    if (K <= 0 || !(temperature > 0.0f) || !(temperature <= FLT_MAX)) return SPECS_ERR_SHAPE;
+    if (K <= 0 || !good_temperature(temperature)) return SPECS_ERR_SHAPE;
     if (K > kMaxTopLogits) return SPECS_ERR_LIMIT;
     if (rows == 0) return SPECS_OK;
     if (!top_ids || !top_values) return SPECS_ERR_NULL;
@@ -662,7 +665,7 @@ static int check_distill(specs_ctx* ctx, const void* logits, int dtype, int64_t 
     if (!ctx) return SPECS_ERR_NULL;
     int st = check_rows(logits, dtype, row_stride, rows, V);
     if (st != SPECS_OK) return st;
-    if (K <= 0 || !(temperature > 0.0f) || !(temperature <= FLT_MAX)) return SPECS_ERR_SHAPE;
+    if (K <= 0 || !good_temperature(temperature)) return SPECS_ERR_SHAPE;
     if (K > kMaxTopLogits) return SPECS_ERR_LIMIT;
     if (with_grad && rows > 1 && grad_stride < V) return SPECS_ERR_SHAPE;      // rows of the gradient are written
     if (rows == 0) return SPECS_OK;
