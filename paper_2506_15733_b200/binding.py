@@ -193,6 +193,11 @@ def device_arg(t, dtype: str, count: int, device: int, name: str) -> Optional[in
     return t.data_ptr()
 
 
+def _int32_size(n: int) -> int:
+    """A size for an int32 argument: one beyond its range stays beyond every limit instead of losing its upper bits."""
+    return min(n, 0x7fffffff)
+
+
 def rows_arg(t, device: int, name: str):
     """(address, dtype code, row stride, rows, V) of a matrix of logits: float32, bfloat16 or float16, rows any number
     of elements apart, the elements of a row contiguous.  Raises TypeError or ValueError like ``device_arg``."""
@@ -212,13 +217,13 @@ def rows_arg(t, device: int, name: str):
         raise ValueError(f"{name}: the elements of a row are not contiguous")
     if t.get_device() != device:
         raise ValueError(f"{name}: tensor is on {t.device}, the context is on cuda:{device}")
-    return t.data_ptr(), code, stride, rows, V
+    return t.data_ptr(), code, stride, rows, _int32_size(V)
 
 
 def _list_length(t, name: str) -> int:
     if getattr(t, "dim", lambda: 0)() != 2:
         raise ValueError(f"{name}: expected [rows, K]")
-    return t.shape[1]
+    return _int32_size(t.shape[1])
 
 
 def _pitched(t, per_row: int, name: str):
