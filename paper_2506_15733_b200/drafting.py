@@ -76,18 +76,22 @@ class _DistillLoss(torch.autograd.Function):
         lse = lists.lse if with_rest else None
         ctx.specs_distill_forward(logits, lists.ids, lists.values, loss, stats, temperature=lists.temperature,
                                   top_lse=lse, row_weight=row_weight)
-        fn.save_for_backward(logits, stats)
-        fn.rest = (ctx, lists, lse, row_weight)
+        # torch watches over what it saves; tensors of inference mode (a teacher's, often) it does not save
+        given = (lists.ids, lists.values, lse, row_weight)
+        watched = [t is not None and not t.is_inference() for t in given]
+        fn.save_for_backward(logits, stats, *(t if w else None for t, w in zip(given, watched)))
+        fn.rest = (ctx, lists.temperature, [None if w else t for t, w in zip(given, watched)])
         return loss
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(fn, grad_loss):
-        logits, stats = fn.saved_tensors
-        ctx, lists, lse, row_weight = fn.rest
+        logits, stats, *watched = fn.saved_tensors
+        ctx, temperature, others = fn.rest
+        ids, values, lse, row_weight = (o if w is None else w for w, o in zip(watched, others))
         grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        ctx.specs_distill_backward(logits, lists.ids, lists.values, stats, grad, temperature=lists.temperature,
-                                   top_lse=lse, row_weight=row_weight, grad_loss=grad_loss.float().contiguous())
+        ctx.specs_distill_backward(logits, ids, values, stats, grad, temperature=temperature, top_lse=lse,
+                                   row_weight=row_weight, grad_loss=grad_loss.float().contiguous())
         return grad, None, None, None, None
 
 
@@ -95,5 +99,11 @@ def distill_loss(ctx: "binding.Context", logits: torch.Tensor, lists: TeacherLis
                  row_weight: Optional[torch.Tensor] = None) -> torch.Tensor:
     """float32 [rows]: the divergence of softmax(logits / T) from the teacher's lists, differentiable with respect to
     ``logits``.  ``with_rest``: the mass that a list leaves out is one more outcome; otherwise the lists are normalised by
-    themselves.  The logits must not be changed between the forward and the backward pass (torch checks)."""
+    themselves.  Neither the logits nor the lists and weights may be changed between the forward and the backward pass
+    (torch checks).  There is no gradient with respect to lists and weights: what requires one is refused."""
+    if torch.is_grad_enabled():
+        for name, t in (("lists.values", lists.values), ("lists.lse", lists.lse if with_rest else None),
+                        ("row_weight", row_weight)):
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{name} requires a gradient, and there is no gradient with respect to it: detach it")
     return _DistillLoss.apply(logits, ctx, lists, with_rest, row_weight)
