@@ -33,7 +33,7 @@ constexpr int kListCap = 2048, kPer = kListCap / kThreads;   // entries of the f
 constexpr int kMassBins = 1024, kCoarse = 64, kFine = kMassBins / kCoarse;
 constexpr float kBinsPerUnit = 45.0f;        // bins per unit of the exponent: weights end at 22.2, bin 999
 constexpr int kBins = 64, kMaxLevels = 12;   // narrowing: 32 bits of a key and 19 of an id, 6 a level, take 10 at most
-constexpr int kTargetCtas = 296, kLeastUnits = 1024, kLongUnits = 16384;
+constexpr int kLeastUnits = 1024, kLongUnits = 16000;
 constexpr uint32_t kHighestKey = 0xffffffffu, kKeyOfMinusZero = 0x7fffffffu;   // order_key has both zeros at 0x80000000
 
 // Temperature in the exponent.  NaN and what is too small to weigh anything become -30, so that no special case remains.
@@ -973,14 +973,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_kernel(const SampleAr
 // bf16, nothing cut off / nucleus / top-k (us): 111 rows on 222 CTAs 26 / 36 / 15, on 444 37 / 54 / 24; 256 rows on 256 CTAs
 // 34 / 45 / 16, on 512 45 / 64 / 26; 60 rows of 151936 on 240 38 / 51 / 18, on 480 50 / 74 / 27.  With 256 or 512 units a CTA
 // the exchanges cost more than the shorter passes save (37 x 32003 fp16, nucleus: 35 us instead of 26).
-// Rows of more than 16384 units get two CTAs all the same, where no more than 296 are at work: batches of mixed settings leave
-// SMs idle behind their longest rows (256 x 151936: 86 us instead of 96; of one setting 108 / 143 / 40 instead of 106 / 126 / 31).
-int cluster_size(int64_t rows, int units) {
+// Rows of 16000 units and more get two CTAs as long as there are no more than 3/2 of them an SM: with one each, half of the SMs or
+// more would have a single CTA, and a long row takes long.  Measured with one / two (us, nothing cut off, nucleus, top-k, min-p,
+// and the four of them mixed): 128256 bf16, 210 rows 88 119 34 73 88 / 80 109 42 73 65, 230 rows 86 116 35 73 88 / 89 114 42 86 73;
+// 151936 bf16, 170 rows 100 137 37 85 88 / 88 115 40 81 68, 256 rows 105 143 40 87 103 / 105 135 48 99 89; 65536 bf16, 170 rows
+// 47 62 24 44 44 / 51 67 30 48 40.
+int cluster_size(int64_t rows, int units, int num_sms) {
     int ranks = 1;
-    while (ranks < kMaxCluster && units > ranks * kLeastUnits &&
-           (rows * 2 * ranks <= kTargetCtas || (rows <= kTargetCtas && units > ranks * kLongUnits)))
-        ranks *= 2;
-    return ranks;
+    while (ranks < kMaxCluster && units > ranks * kLeastUnits && rows * 2 * ranks <= 2 * num_sms) ranks *= 2;
+    return ranks == 1 && units >= kLongUnits && 2 * rows <= 3 * num_sms ? 2 : ranks;
 }
 
 template <typename Args>
@@ -1011,7 +1012,7 @@ bool prepare_pick_rows() {
 }
 
 int launch_sample_rows(const SampleArgs& a, int dtype, cudaStream_t stream) {
-    const int ranks = cluster_size(a.rows, a.V / (dtype == SPECS_F32 ? 4 : 8));
+    const int ranks = cluster_size(a.rows, a.V / (dtype == SPECS_F32 ? 4 : 8), a.num_sms);
     return launch(dtype == SPECS_F32 ? sample_rows_kernel<float>
                   : dtype == SPECS_BF16 ? sample_rows_kernel<__nv_bfloat16> : sample_rows_kernel<__half>, a, ranks, stream);
 }
@@ -1024,7 +1025,7 @@ int launch_sample_rows(const SampleArgs& a, int dtype, cudaStream_t stream) {
 int launch_top_rows(const TopArgs& a, int dtype, cudaStream_t stream) {
     if (a.rows > a.num_sms && a.V / (dtype == SPECS_F32 ? 4 : 8) >= kStreamUnits && a.K <= kStreamTop)
         return launch_top_stream(a, dtype, stream);
-    const int ranks = cluster_size(a.rows, a.V / (dtype == SPECS_F32 ? 4 : 8));
+    const int ranks = cluster_size(a.rows, a.V / (dtype == SPECS_F32 ? 4 : 8), a.num_sms);
     return launch(dtype == SPECS_F32 ? top_rows_kernel<float>
                   : dtype == SPECS_BF16 ? top_rows_kernel<__nv_bfloat16> : top_rows_kernel<__half>, a, ranks, stream);
 }
