@@ -638,7 +638,7 @@ int specs_sample_tokens(specs_ctx* ctx, const void* logits, int dtype, int64_t r
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return SPECS_ERR_CUDA;
     const SampleArgs a = {logits, row_stride, rows, V, temperature, top_k, top_p, min_p, uniforms, tokens, tok_logprob,
-                          draw_logprob, ctx->num_sms};
+                          draw_logprob, ctx->d_status, ctx->num_sms};
     return launch_sample_rows(a, dtype, static_cast<cudaStream_t>(cuda_stream));
 }
 

@@ -62,6 +62,7 @@ __device__ uint32_t mark_listed(const DistillArgs& a, int64_t r, const Slice<T>&
         if (id >= a.V) s.bad = 1;
         const int i = slice.index_of(id);
         if (i < 0) continue;
+        if (!SPECS_IN_BOUNDS(i, slice.count(), a.status)) continue;
         const uint32_t bit = 1u << ((i & 3) * 8 + (id + slice.row.lead) % Elem<T>::kWidth);
         if (atomicOr(&listed_bits[i >> 2], bit) & bit) s.twice = 1;
         else first |= mine;
@@ -82,7 +83,7 @@ __device__ void list_sums(const DistillArgs& a, int64_t r, const Slice<T>& slice
         const int id = ids[j];
         if (missing(id)) continue;
         most = fmaxf(most, t[j]);
-        if (!student) continue;
+        if (!student || !SPECS_IN_BOUNDS(id, a.V, a.status) || !SPECS_IN_BOUNDS(j, kMaxTopLogits, a.status)) continue;
         const float logit = Elem<T>::to_float(slice.row.row[id]);
         s.listed_logit[j] = logit;
         near = fmaxf(near, logit);
@@ -121,7 +122,7 @@ __device__ __forceinline__ void first_batch(const Slice<T>& slice, uint4* q) {
 
 // One pass over the slice, the first batch being there already: the warp's sums.
 template <typename T>
-__device__ __forceinline__ void read_slice(const Slice<T>& slice, uint4* q, float c, bool lists, Part& part) {
+__device__ __forceinline__ void read_slice(const DistillArgs& a, const Slice<T>& slice, uint4* q, bool lists, float c, Part& part) {
     RunningSums<T> sums(c);
     const int step = slice.step;
     int u = slice.start(threadIdx.x), i = threadIdx.x;
@@ -129,7 +130,10 @@ __device__ __forceinline__ void read_slice(const Slice<T>& slice, uint4* q, floa
         constexpr int kUnits = decltype(count)::value;
         uint32_t bits[kUnits];
 #pragma unroll
-        for (int j = 0; j < kUnits; ++j) bits[j] = lists ? unit_bits(i + j * kStreamers) : 0;
+        for (int j = 0; j < kUnits; ++j) {
+            const int at = i + j * kStreamers;
+            bits[j] = lists && SPECS_IN_BOUNDS(at, padded_units(slice.count()), a.status) ? unit_bits(at) : 0;
+        }
         sums.template add<kUnits>(units, [&](int j) { return bits[j] != 0; }, [&](int j) { return bits[j]; });
     };
     if (u < slice.end) {
@@ -233,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_rows_kernel(const
                     if (slice.index_of(id) >= 0) s.listed_logit[j] = Elem<T>::to_float(slice.row.row[id]);
                 }
         } else if (kMode != kBackward) {
-            read_slice(slice, q, c, a.top_lse != nullptr, part);
+            read_slice(a, slice, q, a.top_lse != nullptr, c, part);
             if ((threadIdx.x & 31) == 0) {
                 const int w = threadIdx.x >> 5;
                 s.top[w] = part.top;
@@ -284,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_rows_kernel(const
     __syncthreads();
     for (int j = threadIdx.x; j < a.K; j += kThreads) {    // then the listed ones over it
         const int id = a.top_ids[r * a.K + j];
-        if (slice.index_of(id) < 0) continue;
+        if (slice.index_of(id) < 0 || !SPECS_IN_BOUNDS(id, a.V, a.status)) continue;
         float q_id = 0.0f;
         if (s.twice) {
             for (int i = 0; i < a.K; ++i)

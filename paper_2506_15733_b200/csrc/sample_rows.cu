@@ -93,12 +93,20 @@ struct Shared {
     uint32_t count, flagged, in_bin, complete;
     Interval at;
     uint64_t found_place, found_before, allowed, total;
+    uint32_t* status;                                        // of the checked build
 };
 
 // By this name, and not by a reference handed down, so that out-of-line functions know that it is shared memory.
 __device__ __forceinline__ Shared& shared() {
     extern __shared__ __align__(16) uint8_t smem[];
     return *reinterpret_cast<Shared*>(smem);
+}
+
+// The checked build's index checks report to the status word, which functions find in shared memory.  (Before the first barrier.)
+__device__ __forceinline__ void report_to(Shared& s, uint32_t* status) {
+#ifdef SPECS_DEBUG
+    if (threadIdx.x == 0) s.status = status;
+#endif
 }
 
 // What a thread knows of its row's cluster.
@@ -199,6 +207,7 @@ __device__ float log_row_sum(const Cluster& c, const Shared& s, const RowPart& r
 // the threads sharing out the comparisons (256 entries: 64 16-byte loads a thread).  More: bitonic.
 __device__ __noinline__ void sort_list(int n) {
     Shared& s = shared();
+    if (!SPECS_IN_BOUNDS(n, kListCap + 1, s.status)) return;
     const int tid = threadIdx.x;
     int size = 32;
     while (size < n) size <<= 1;
@@ -221,7 +230,7 @@ __device__ __noinline__ void sort_list(int n) {
         __syncthreads();
         const uint32_t at = tid < n ? rank[tid] : 0;
         __syncthreads();
-        if (tid < n) list[at] = v;                           // places are distinct, and so are the ranks
+        if (tid < n && SPECS_IN_BOUNDS(at, n, s.status)) list[at] = v;     // places are distinct, and so are the ranks
     } else if (size <= kThreads) {
         // a thread holds one entry: partners less than a warp apart swap by shuffles
         uint64_t v = list[tid];
@@ -280,15 +289,16 @@ __device__ V block_before(V v, V* scratch, V* total) {
 }
 
 // ---- the list -----------------------------------------------------------------------------------
-__device__ __forceinline__ void push_entry(Shared& s, Shared* home, uint32_t key, int id) {
+__device__ __forceinline__ void push_entry(Shared& s, Shared* home, uint32_t key, int id, int V) {
+    if (!SPECS_IN_BOUNDS(id, V, s.status)) return;
     atomicAdd(&s.count, 1u);
     const uint32_t pos = atomicAdd(&home->filled, 1u);
     if (pos < kListCap) home->list[pos] = place_of(key, id);
 }
 
 template <typename T>
-__device__ __forceinline__ void push_unit(Shared& s, Shared* home, const uint4& q, int id, uint32_t lo, uint32_t hi, int first,
-                                          int last) {
+__device__ __forceinline__ void push_unit(Shared& s, Shared* home, int V, const uint4& q, int id, uint32_t lo, uint32_t hi,
+                                          int first, int last) {
     // (as numbers; an interval that ends at the key of -0, which no entry has, ends at the number below the zeros)
     const float least = key_value(lo), most = hi == kHighestKey ? INFINITY : key_value(hi == kKeyOfMinusZero ? hi - 1 : hi);
     float f[Elem<T>::kWidth];
@@ -302,7 +312,7 @@ __device__ __forceinline__ void push_unit(Shared& s, Shared* home, const uint4& 
         float v = f[0];
 #pragma unroll
         for (int k = 1; k < Elem<T>::kWidth; ++k) v = e == k ? f[k] : v;
-        if (id + e >= first && id + e <= last) push_entry(s, home, order_key(v), id + e);
+        if (id + e >= first && id + e <= last) push_entry(s, home, order_key(v), id + e, V);
     }
 }
 
@@ -320,21 +330,25 @@ __device__ __noinline__ uint32_t push_entries(const Cluster c, const Slice<T> sl
     if (hi == kHighestKey) {
 #pragma unroll
         for (int j = 0; j < kGroups; ++j)
-            if (st.group_key[j] >= lo) s.flags[atomicAdd(&s.flagged, 1u)] = (uint16_t)(threadIdx.x * kGroups + j);
+            if (st.group_key[j] >= lo) {
+                const uint32_t at = atomicAdd(&s.flagged, 1u);
+                if (SPECS_IN_BOUNDS(at, kThreads * kGroups, s.status)) s.flags[at] = (uint16_t)(threadIdx.x * kGroups + j);
+            }
         __syncthreads();
         const int per = (slice.row.units + kGroups * slice.step - 1) / (kGroups * slice.step);   // units of a group, at most
         const int work = (int)s.flagged * per;
         for (int w = threadIdx.x; w < work; w += kThreads) {
             const int flag = s.flags[w / per], n = w % per;
             const int u = slice.start(flag / kGroups) + (n * kGroups + flag % kGroups) * slice.step;
-            if (u < slice.row.units) push_unit<T>(s, home, slice.row.load(u), slice.row.first(u), lo, hi, first, last);
+            if (u < slice.row.units && SPECS_IN_BOUNDS(u, slice.row.units, s.status))
+                push_unit<T>(s, home, slice.row.V, slice.row.load(u), slice.row.first(u), lo, hi, first, last);
         }
     } else {
         slice.template each_batch<kGroups>([&](const uint4* q, int u) {
 #pragma unroll 1
             for (int j = 0; j < kGroups; ++j)
-                push_unit<T>(s, home, j == 0 ? q[0] : j == 1 ? q[1] : j == 2 ? q[2] : q[3], slice.row.first(u + j * slice.step), lo,
-                             hi, first, last);
+                push_unit<T>(s, home, slice.row.V, j == 0 ? q[0] : j == 1 ? q[1] : j == 2 ? q[2] : q[3],
+                             slice.row.first(u + j * slice.step), lo, hi, first, last);
         });
     }
     __syncthreads();
@@ -355,6 +369,7 @@ __device__ __forceinline__ void weigh_list(Shared& s, int n, float top, float in
 // left.  s.found_before gets the list's mass before it.
 __device__ __noinline__ void narrow_list(int n, bool by_mass, uint64_t goal) {
     Shared& s = shared();
+    if (!SPECS_IN_BOUNDS(n, kListCap + 1, s.status)) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t live = 0;
     __syncthreads();                                         // the weights are there
@@ -393,6 +408,7 @@ __device__ __noinline__ void narrow_list(int n, bool by_mass, uint64_t goal) {
                 const uint64_t place = s.list[threadIdx.x + i * kThreads];
                 const uint32_t w = s.weight[threadIdx.x + i * kThreads];
                 digit[i] = (by_key ? most - place_key(place) : (uint32_t)place_id(place) - first) >> shift;
+                if (!SPECS_IN_BOUNDS(digit[i], kBins, s.status)) continue;
                 atomicAdd(&s.narrow.count[digit[i]], 1u);
                 atomicAdd(&s.narrow.low[digit[i]], w & 0xffffu);
                 if (w >> 16) atomicAdd(&s.narrow.high[digit[i]], w >> 16);
@@ -516,6 +532,7 @@ __device__ __noinline__ void search(const Cluster c, const Slice<T> slice, const
                 const int id = slice.row.first(u) + e;
                 if (key < at.lo || key > at.hi || id < at.first || id > at.last) continue;
                 const uint32_t d = (by_key ? at.hi - key : (uint32_t)(id - at.first)) >> shift;
+                if (!SPECS_IN_BOUNDS(d, kBins, s.status)) continue;
                 const uint32_t w = weight_of(scaled(v, top, inv_t));
                 atomicAdd(&s.h.count[d][lane], 1u);
                 atomicAdd(&s.h.low[d][lane], w & 0xffffu);   // a column gets a 32nd of the slice: below 2^15 entries
@@ -633,7 +650,8 @@ __device__ void add_masses(const Cluster& c, Shared& s, const Slice<T>& slice, f
 #pragma unroll
             for (int e = 0; e < kWidth; ++e) {
                 sum[e] = 0;
-                if (w[e]) sum[e] = atomicAdd(bin(s.mass.low, __float_as_uint(bits[e])), w[e]);
+                if (w[e] && SPECS_IN_BOUNDS((__float_as_uint(bits[e]) - 0x4a000000u) >> 2, kMassBins, s.status))
+                    sum[e] = atomicAdd(bin(s.mass.low, __float_as_uint(bits[e])), w[e]);
             }
             bool carry = false;
 #pragma unroll
@@ -770,6 +788,7 @@ __global__ void __launch_bounds__(kThreads, 2) top_rows_kernel(const TopArgs a) 
     const int tid = threadIdx.x;
     const int64_t r = blockIdx.x / c.ranks;
     if (tid == 0) s.filled = 0;
+    report_to(s, a.status);
     const Slice<T> slice(static_cast<const T*>(a.logits) + r * a.row_stride, a.V, __ffs(c.ranks) - 1, c.rank);
     const float scale = a.inv_t * kLog2e;
     const Streamed st = stream_slice(slice, a.lse != nullptr, scale, s);
@@ -812,6 +831,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_kernel(const SampleAr
     const int tid = threadIdx.x;
     const int64_t r = blockIdx.x / c.ranks;
     if (tid == 0) { s.filled = 0; s.found_place = 0; s.found_before = 0; }
+    report_to(s, a.status);
 
     // the row's settings
     const float temp = a.temperature ? a.temperature[r] : 1.0f;
@@ -960,7 +980,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_kernel(const SampleAr
         const float l = place ? key_value(place_key(place)) : nan;
         const float ln_sum = log_row_sum(c, s, row, kLog2e);
         if (tid == 0) {
-            a.tokens[r] = place ? place_id(place) : -1;
+            a.tokens[r] = place && SPECS_IN_BOUNDS(place_id(place), a.V, a.status) ? place_id(place) : -1;
             if (a.tok_logprob) a.tok_logprob[r] = (l - top) - ln_sum;
             if (a.draw_logprob)
                 a.draw_logprob[r] = !place ? nan : kept == 0 ? 0.0f

@@ -321,7 +321,7 @@ struct SampleArgs {
     const float* temperature; const int32_t* top_k; const float* top_p; const float* min_p;   // each [rows] or NULL
     const float* uniforms;
     int32_t* tokens; float* tok_logprob; float* draw_logprob;                                  // the last two may be NULL
-    int num_sms;
+    uint32_t* status; int num_sms;
 };
 struct TopArgs {
     const void* logits; int64_t row_stride, rows; int32_t V, K;
