@@ -38,7 +38,7 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     lib = LIB_PATH_DEBUG if debug else LIB_PATH
     if not force and not needs_build(debug):
         return lib
-    cmd = [_nvcc(), "-shared", "-Xcompiler", "-fPIC", "-std=c++17", "-O3", "-lineinfo",
+    cmd = [_nvcc(), "--threads", "0", "-shared", "-Xcompiler", "-fPIC", "-std=c++17", "-O3", "-lineinfo",
            "-gencode", "arch=compute_100a,code=sm_100a",
            "-I", os.path.join(ROOT, "include"), "-I", CSRC,
            "-o", lib] + (["-DSPECS_DEBUG"] if debug else []) + [os.path.join(CSRC, s) for s in SOURCES]
