@@ -51,10 +51,8 @@ __device__ __forceinline__ double teacher_scale(const Part& p, double ref) {
     return p.ref == ref ? 1.0 : p.mass == 0.0 ? 0.0 : exp(p.ref - ref);
 }
 
-// One warp, a part per lane (no_part where there is none): the teacher of the row, in every lane.
-__device__ __forceinline__ void combine_teacher(const DistillArgs& a, const Part& p, Row& row) {
-    const double ref = warp_reduce(p.ref, MaxOp());
-    const double mass = warp_reduce(p.mass * teacher_scale(p, ref), AddOp());
+// The row from sums over all parts.  Teacher:
+__device__ __forceinline__ void set_teacher(const DistillArgs& a, double ref, double mass, Row& row) {
     if (a.top_lse) {
         row.norm = ref;
         row.listed = mass;
@@ -69,29 +67,51 @@ __device__ __forceinline__ void combine_teacher(const DistillArgs& a, const Part
 __device__ __forceinline__ float moved(float from, float to, float c) {
     return from == -INFINITY || from == to ? 1.0f : fast_exp2((from - to) * c);
 }
-// ... the student's listed entries, over all parts: the largest, and the sum relative to it ...
+// Student, after the teacher: the largest listed logit with the sum relative to it, and the same of the unlisted ones.
 struct Listed { float near, sum; };
+__device__ __forceinline__ void set_student(const DistillArgs& a, const Listed& listed, float top, float rest, float c, Row& row) {
+    row.rest_top = top;
+    row.rest_own = rest;
+    row.top = fmaxf(top, listed.near);                     // (without top_lse all of these are in `top`, and listed.sum is 0)
+    row.rest = rest * moved(top, row.top, c);
+    row.sum = row.rest + listed.sum * moved(listed.near, row.top, c);
+    const bool none = rest == 0.0f || ((double)row.top - (double)top) * (double)a.inv_t > kLeastRest;
+    if (none && rest == rest) row.left = 0.0f;             // (NaN stays one)
+}
+
+// One warp, a part per lane (no_part where there is none), the results in every lane: the teacher of the row ...
+__device__ __forceinline__ void combine_teacher(const DistillArgs& a, const Part& p, Row& row) {
+    const double ref = warp_reduce(p.ref, MaxOp());
+    set_teacher(a, ref, warp_reduce(p.mass * teacher_scale(p, ref), AddOp()), row);
+}
+// ... the student's listed entries, and the student with these ...
 __device__ __forceinline__ Listed combine_listed(const Part& p, float c) {
     const float near = warp_reduce(p.near, MaxOp());
     return {near, (float)warp_reduce((double)p.listed * moved(p.near, near, c), AddOp())};
 }
-// ... and the student with these.
 __device__ __forceinline__ void combine_student(const DistillArgs& a, const Part& p, const Listed& listed, float c, Row& row) {
-    row.rest_top = warp_reduce(p.top, MaxOp());
-    row.rest_own = (float)warp_reduce((double)p.rest * moved(p.top, row.rest_top, c), AddOp());
-    row.top = fmaxf(row.rest_top, listed.near);            // (without top_lse all of these are in rest_top, and listed.sum is 0)
-    row.rest = row.rest_own * moved(row.rest_top, row.top, c);
-    row.sum = row.rest + listed.sum * moved(listed.near, row.top, c);
-    const bool none = row.rest_own == 0.0f || ((double)row.top - (double)row.rest_top) * (double)a.inv_t > kLeastRest;
-    if (none && row.rest_own == row.rest_own) row.left = 0.0f;         // (NaN stays one)
+    const float top = warp_reduce(p.top, MaxOp());
+    set_student(a, listed, top, (float)warp_reduce((double)p.rest * moved(p.top, top, c), AddOp()), c, row);
+}
+// ... or all at once.
+__device__ __forceinline__ void combine_row(const DistillArgs& a, const Part& p, float c, Row& row) {
+    double ref = p.ref;
+    float top = p.top, near = p.near;
+    warp_maxima(ref, top, near);
+    double mass = p.mass * teacher_scale(p, ref), rest = (double)p.rest * moved(p.top, top, c),
+           listed = (double)p.listed * moved(p.near, near, c);
+    warp_sums(mass, rest, listed);
+    set_teacher(a, ref, mass, row);
+    set_student(a, {near, (float)listed}, top, (float)rest, c, row);
 }
 
 // What the forward pass leaves of the unlisted part for the backward pass: itself, or its logarithm where it is below the normal
 // floats (which is negative, while it is not); 0 where it does not count.
 __device__ __forceinline__ float rest_to_stats(const DistillArgs& a, const Row& row) {
-    const double down = ((double)row.rest_top - (double)row.top) * (double)a.inv_t;
     if (!a.top_lse || row.rest_own == 0.0f) return 0.0f;
+    if (row.rest >= kNearRest) return row.rest;
     if (row.rest_own != row.rest_own) return row.rest_own;
+    const double down = ((double)row.rest_top - (double)row.top) * (double)a.inv_t;
     if (down < -kLeastRest) return 0.0f;
     const double rest = (double)row.rest_own * exp(down);
     return rest < 1.1754943508222875e-38 ? (float)(log((double)row.rest_own) + down) : (float)rest;

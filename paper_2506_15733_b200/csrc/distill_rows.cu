@@ -88,8 +88,8 @@ __device__ void list_sums(const DistillArgs& a, int64_t r, const Slice<T>& slice
         s.listed_logit[j] = logit;
         near = fmaxf(near, logit);
     }
-    most = warp_reduce(most, MaxOp());
-    part.near = student ? warp_reduce(near, MaxOp()) : -INFINITY;
+    warp_maxima(most, near);
+    part.near = near;
     part.ref = a.top_lse ? (double)a.top_lse[r] : (double)most * (double)a.inv_t;
     part.mass = part.cross = 0.0;
     part.lost = -INFINITY;
@@ -106,10 +106,8 @@ __device__ void list_sums(const DistillArgs& a, int64_t r, const Slice<T>& slice
         if (logit == -INFINITY) part.lost = fmaxf(part.lost, t[j]);
         else part.cross += e * (x - ((double)logit - (double)from) * (double)a.inv_t);
     }
-    part.lost = warp_reduce(part.lost, MaxOp());
-    part.listed = warp_reduce(part.listed, AddOp());
-    part.mass = warp_reduce(part.mass, AddOp());
-    part.cross = warp_reduce(part.cross, AddOp());
+    warp_sums(part.listed, part.mass, part.cross);
+    warp_maxima(part.lost);
 }
 
 // ---- the streaming warps ------------------------------------------------------------------------
@@ -271,8 +269,7 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_rows_kernel(const
     const int lane = threadIdx.x & 31;
     const Part mine = lane < (kMode == kBackward ? 1 : ranks) ? s.part[lane] : no_part();
     Row row;
-    combine_teacher(a, mine, row);
-    if (kMode != kBackward) combine_student(a, mine, combine_listed(mine, c), c, row);
+    if (kMode != kBackward) combine_row(a, mine, c, row); else combine_teacher(a, mine, row);
     if (kMode == kBackward) student_from_stats(a, r, row);
     if (kMode != kBackward && lists && rank == 0) {
         const float loss = row_loss(a, mine, row);

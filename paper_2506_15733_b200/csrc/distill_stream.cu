@@ -197,8 +197,7 @@ __device__ void load_list(const DistillArgs& a, int64_t r, Slot& slot, uint32_t*
 #pragma unroll
     for (int i = 0; i < kPer; ++i) near = fmaxf(near, logit[i]);
     Part part = no_part();
-    most = warp_reduce(most, MaxOp());
-    near = warp_reduce(near, MaxOp());
+    warp_maxima(most, near);
     part.near = near;
     near = finite_or_zero(near);
     part.ref = a.top_lse ? (double)a.top_lse[r] : (double)most * (double)a.inv_t;
@@ -212,9 +211,8 @@ __device__ void load_list(const DistillArgs& a, int64_t r, Slot& slot, uint32_t*
         if (logit[i] == -INFINITY) part.lost = fmaxf(part.lost, value[i]);
         else part.cross += e * (x - ((double)logit[i] - (double)near) * (double)a.inv_t);
     }
-    part.lost = warp_reduce(part.lost, MaxOp());
-    part.mass = warp_reduce(part.mass, AddOp());
-    part.cross = warp_reduce(part.cross, AddOp());
+    warp_sums(part.mass, part.cross);
+    warp_maxima(part.lost);
     if (lane == 0) slot.part[warp] = part;
     listers_meet();
     if (kMode != kBackward && a.top_lse) {                 // the student's sum over the listed ids, each of them once

@@ -306,5 +306,16 @@ __device__ __forceinline__ V warp_reduce(V v, Op op) {
 }
 struct MaxOp { template <typename V> __device__ V operator()(V a, V b) const { return a > b ? a : b; } };
 struct AddOp { template <typename V> __device__ V operator()(V a, V b) const { return a + b; } };
+// Several at a time: their shuffles do not wait for one another.
+template <typename... V>
+__device__ __forceinline__ void warp_maxima(V&... v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ((v = MaxOp()(v, __shfl_xor_sync(kAllLanes, v, o))), ...);
+}
+template <typename... V>
+__device__ __forceinline__ void warp_sums(V&... v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ((v += __shfl_xor_sync(kAllLanes, v, o)), ...);
+}
 
 }  // namespace specs
