@@ -409,8 +409,9 @@ int specs_beam_step_fp8(specs_ctx* ctx, const void* hidden, const uint8_t* W_q, 
  *               padded LM head, 0 for one row read by all) and any alignment that the element type allows.
  *   V           at most SPECS_MAX_ROW_VOCAB, rows at most SPECS_MAX_LOGIT_ROWS (SPECS_ERR_LIMIT).
  * A logit of -inf is a masked entry: it has no probability and is never drawn or listed.  Masks of the
- * type's lowest finite value work too, as the very small numbers they are.  Sums are fp32
- * per thread and warp and fp64 (or whole numbers) above that.  Ids depend on nothing but their row; the number of rows
+ * type's lowest finite value work too, as the very small numbers they are.  The sampler's masses are whole numbers.
+ * Sums of exponentials are fp32 within a warp, and over a CTA's 16 warps in specs_sample_tokens and specs_top_logits;
+ * above that they are fp64, as the teacher's sums are throughout.  They are good to about 3e-5 of themselves.  Ids depend on nothing but their row; the number of rows
  * and their alignment decide how a row is shared out, so that a sum's last bit may differ with them.  The same call
  * gives the same bits again. */
 #define SPECS_F32  0
@@ -433,7 +434,7 @@ int specs_beam_step_fp8(specs_ctx* ctx, const void* hidden, const uint8_t* W_q, 
  * With Z the mass that is left, the token is the first entry at which the running mass exceeds
  * floor(uniform * Z): an exact draw, to steps of 2^-24 of the uniform, in which small uniforms give likely tokens.
  *   temperature  float [rows] T; T <= 0, NaN, or so small that 1 / T overflows takes the
-                largest logit (lowest id among equals).
+ *                largest logit (lowest id among equals).
  *   uniforms     float [rows] in [0, 1); values outside are clamped.
  *   tokens       int32 [rows] out; -1 for a row without a logit above -inf.
  *   tok_logprob  float [rows] out or NULL: log pi of the token under the model itself, the softmax of all V

@@ -8,8 +8,10 @@
 // gradient pass of specs_distill_step then reads the slice again: the CTAs of a row are in flight together, so the second
 // read comes from L2, and HBM sees each logit once in and each gradient once out.
 //
-// Bound: a launch and the exchange for small rows (64 x 1024 fp32 forward 4.7 us), then a CTA's share of a row: 592 rows of
-// 16384 bf16, forward 12 us, 1.6 TB/s, step 17 us, 2.3 TB/s.
+// Bound: a launch and the exchange for small rows (64 x 1024 fp32 forward 4.6 us, with the remaining mass 5.3), then the latency of
+// a CTA's steps, list and stream in turn, for its share of a row: 592 rows of 16384 bf16, forward 13 us, 1.5 TB/s, step 15 us,
+// 2.6 TB/s.  A gradient whose rows lie otherwise on 16-byte boundaries than the logits' is written element by element: 592 x 16384,
+// backward 13 -> 45 us, step 15 -> 47; 37 x 131072, 7 -> 20 and 11 -> 30.
 #include <cooperative_groups.h>
 
 #include "distill.cuh"
@@ -330,8 +332,9 @@ bool prepare_typed() {
 }
 
 // One persistent CTA per SM (distill_stream.cu) for more rows than SMs that are long enough for its lists to be fetched behind
-// them.  Measured, clusters / streamed, forward, backward and step (us): 131072 bf16, 180 rows 23 / 21, 28 / 24, 41 / 40; 1184 rows
-// 74 / 64, 120 / 113, 171 / 138; 65536, 592 rows 28 / 27, 41 / 31, 49 / 49; 32768, 592 rows 16 / 21, 24 / 24, 28 / 35.
+// them.  Measured, clusters / streamed, forward, backward and step (us): 131072 bf16, 180 rows 22 / 24, 27 / 25, 39 / 42; 1184 rows
+// 72 / 67, 118 / 115, 170 / 142; 98304, 1184 rows 59 / 56, 93 / 89, 128 / 118; 65536, 592 rows 29 / 30, 40 / 33, 47 / 52; 32768, 592
+// rows 19 / 28, 23 / 26, 26 / 37; 49152 fp32, 592 rows 34 / 29, 52 / 45, 71 / 56.
 template <int kMode>
 int launch(const DistillArgs& a, int dtype, cudaStream_t stream) {
     const int units = a.V / (dtype == SPECS_F32 ? 4 : 8);

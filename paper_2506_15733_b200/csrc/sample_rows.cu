@@ -19,8 +19,10 @@
 //   Where a list would be too long (ties, nearly flat rows, a top-k beyond 1024), the cluster narrows the interval of
 //   keys, then of ids, by counting in 64 bins a level.
 //
-// Bound: for few rows the chain of steps, 1 to 4 us each (1 x 151936 bf16 with top-k and nucleus 12 us; 16 x 151936 fp32,
-// nothing cut off, 25 us); for many the second pass's arithmetic (256 x 151936 bf16, mixed settings: 86 us).
+// Bound: for few rows the chain of steps.  1 x 151936 bf16 with top-k and nucleus 12 us: pass 2.5, exchange 2.1, list 2.5, sort 2.1,
+// draw 1.4.  16 x 151936 fp32, nothing cut off, 24 us: pass 2.5, exchange 1.4, masses 7.1, bin 2.8, list 2.8, narrowing 1.7.  For many
+// the two passes over the row: 256 x 151936 bf16, mixed settings, 95 us, of which a row without top-k takes 70 (pass 16, masses 40 to
+// 45, the search 7 to 10), one with top-k 25, and a greedy one 35 (14 of them listing the largest among its own units again).
 #include "row_picks.cuh"
 
 namespace specs {
@@ -609,7 +611,7 @@ __device__ __noinline__ void search(const Cluster c, const Slice<T> slice, const
 // The CTA's weights, added up by bins of their exponent, and the sums of kFine bins at a time sent to every CTA.  With
 // `allowed` the mass of the entries that min_p allows, with `weighted` the number of entries that weigh anything.
 // A bin's 32 bits wrap; whoever makes them wrap, as the atomic's result tells, adds a carry: exact, and one atomic an entry
-// where sums of halves take two (151936 bf16 x 256 rows, mixed settings: 103 us with halves and expf).
+// where sums of halves take two (151936 bf16 x 256 rows, mixed settings, on two CTAs each: 86 us, with halves and expf 103).
 // Bound: about 20 instructions per entry.
 template <typename T>
 __device__ void add_masses(const Cluster& c, Shared& s, const Slice<T>& slice, float top, float inv_t, float low,
@@ -1039,8 +1041,8 @@ int launch_sample_rows(const SampleArgs& a, int dtype, cudaStream_t stream) {
 
 // Many rows stream through one persistent CTA per SM (top_stream.cu) as soon as there are more of them than SMs, if they have as
 // many units as that kernel has half its groups, and lists that half of those can bound.  Measured, 16384 and 131072 bf16 (us,
-// clusters / streamed): 148 rows K = 64 13 / 12 and 17 / 17, 200 rows 19 / 13 and 25 / 22, 1184 rows 38 / 28 and 85 / 64,
-// with K = 512 99 / 56 and 162 / 101; against it 296 rows, which clusters take in one wave: 12 / 13 and 23 / 25.  8192 entries
+// clusters / streamed): 148 rows K = 64 13 / 12 and 17 / 17, 200 rows 19 / 12 and 25 / 24, 1184 rows 38 / 27 and 85 / 65,
+// with K = 512 99 / 56 and 162 / 104; against it 296 rows, which clusters take in one wave: 12 / 13 and 23 / 25.  8192 entries
 // are too few for K = 512: 48 / 244, most rows there being listed as ties.
 int launch_top_rows(const TopArgs& a, int dtype, cudaStream_t stream) {
     if (a.rows > a.num_sms && a.V / (dtype == SPECS_F32 ? 4 : 8) >= kStreamUnits && a.K <= kStreamTop)
