@@ -653,8 +653,8 @@ int specs_top_logits(specs_ctx* ctx, const void* logits, int dtype, int64_t row_
     if (!top_ids || !top_values) return SPECS_ERR_NULL;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return SPECS_ERR_CUDA;
-    const TopArgs a = {logits, row_stride, rows, V, K, 1.0f / temperature, top_ids, top_values, lse,
-                       ctx->d_status, ctx->num_sms};
+    const TopArgs a = {logits, row_stride, rows, V, K, 1.0f / temperature, 1.0 / temperature, top_ids, top_values,
+                       lse, ctx->d_status, ctx->num_sms};
     return launch_top_rows(a, dtype, static_cast<cudaStream_t>(cuda_stream));
 }
 
@@ -685,8 +685,8 @@ int specs_distill_forward(specs_ctx* ctx, const void* logits, int dtype, int64_t
     if (!loss) return SPECS_ERR_NULL;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return SPECS_ERR_CUDA;
-    const DistillArgs a = {logits, row_stride, rows, V, K, top_ids, top_values, top_lse, 1.0f / temperature, row_weight,
-                           nullptr, loss, stats, nullptr, 0, ctx->d_status, ctx->num_sms};
+    const DistillArgs a = {logits, row_stride, rows, V, K, top_ids, top_values, top_lse, 1.0f / temperature, 1.0 / temperature,
+                           row_weight, nullptr, loss, stats, nullptr, 0, ctx->d_status, ctx->num_sms};
     return launch_distill_forward(a, dtype, static_cast<cudaStream_t>(cuda_stream));
 }
 
@@ -700,8 +700,8 @@ int specs_distill_backward(specs_ctx* ctx, const void* logits, int dtype, int64_
     if (!stats) return SPECS_ERR_NULL;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return SPECS_ERR_CUDA;
-    const DistillArgs a = {logits, row_stride, rows, V, K, top_ids, top_values, top_lse, 1.0f / temperature, row_weight,
-                           grad_loss, nullptr, const_cast<float*>(stats), grad_logits, grad_stride, ctx->d_status, ctx->num_sms};
+    const DistillArgs a = {logits, row_stride, rows, V, K, top_ids, top_values, top_lse, 1.0f / temperature, 1.0 / temperature,
+                           row_weight, grad_loss, nullptr, const_cast<float*>(stats), grad_logits, grad_stride, ctx->d_status, ctx->num_sms};
     return launch_distill_backward(a, dtype, static_cast<cudaStream_t>(cuda_stream));
 }
 
@@ -715,8 +715,8 @@ int specs_distill_step(specs_ctx* ctx, const void* logits, int dtype, int64_t ro
     if (!loss) return SPECS_ERR_NULL;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return SPECS_ERR_CUDA;
-    const DistillArgs a = {logits, row_stride, rows, V, K, top_ids, top_values, top_lse, 1.0f / temperature, row_weight,
-                           grad_loss, loss, nullptr, grad_logits, grad_stride, ctx->d_status, ctx->num_sms};
+    const DistillArgs a = {logits, row_stride, rows, V, K, top_ids, top_values, top_lse, 1.0f / temperature, 1.0 / temperature,
+                           row_weight, grad_loss, loss, nullptr, grad_logits, grad_stride, ctx->d_status, ctx->num_sms};
     return launch_distill_step(a, dtype, static_cast<cudaStream_t>(cuda_stream));
 }
 

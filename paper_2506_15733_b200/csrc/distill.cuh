@@ -41,9 +41,12 @@ struct Row { float top, sum, rest, rest_top, rest_own, left; double norm, listed
 constexpr double kLeastRest = 690.0;                       // exp() of it: 1e-300, well inside the range of a double
 constexpr float kNearRest = 1e-17f;                        // `rest` from here on: fp32 relative to the row's largest logit will do
 
+// A logit over T, rounded by itself: fused into a difference, a lowest value's would not be that of its equals.
+__device__ __forceinline__ double over_t(const DistillArgs& a, float v) { return __dmul_rn((double)v, a.inv_t64); }
+
 // q_j for the gradient: the exponent in 64 bits, rounded once.
-__device__ __forceinline__ float teacher_q(float t, float inv_t, double norm) {
-    return expf((float)((double)t * (double)inv_t - norm));
+__device__ __forceinline__ float teacher_q(const DistillArgs& a, float t, double norm) {
+    return expf((float)(over_t(a, t) - norm));
 }
 
 // The factor that takes a part's teacher sums to the row's reference.
@@ -75,7 +78,7 @@ __device__ __forceinline__ void set_student(const DistillArgs& a, const Listed& 
     row.top = fmaxf(top, listed.near);                     // (without top_lse all of these are in `top`, and listed.sum is 0)
     row.rest = rest * moved(top, row.top, c);
     row.sum = row.rest + listed.sum * moved(listed.near, row.top, c);
-    const bool none = rest == 0.0f || ((double)row.top - (double)top) * (double)a.inv_t > kLeastRest;
+    const bool none = rest == 0.0f || ((double)row.top - (double)top) * a.inv_t64 > kLeastRest;
     if (none && rest == rest) row.left = 0.0f;             // (NaN stays one)
 }
 
@@ -111,7 +114,7 @@ __device__ __forceinline__ float rest_to_stats(const DistillArgs& a, const Row& 
     if (!a.top_lse || row.rest_own == 0.0f) return 0.0f;
     if (row.rest >= kNearRest) return row.rest;
     if (row.rest_own != row.rest_own) return row.rest_own;
-    const double down = ((double)row.rest_top - (double)row.top) * (double)a.inv_t;
+    const double down = ((double)row.rest_top - (double)row.top) * a.inv_t64;
     if (down < -kLeastRest) return 0.0f;
     const double rest = (double)row.rest_own * exp(down);
     return rest < 1.1754943508222875e-38 ? (float)(log((double)row.rest_own) + down) : (float)rest;
@@ -125,8 +128,8 @@ __device__ __forceinline__ void student_from_stats(const DistillArgs& a, int64_t
         row.left = 0.0f;
     } else if (rest < kNearRest) {                         // relative to a logit about as large as the largest unlisted one
         const double ln_rest = rest < 0.0f ? (double)rest : log((double)rest);
-        row.rest_top = (float)((double)row.top + ln_rest / (double)a.inv_t);
-        row.rest_own = (float)exp(ln_rest - ((double)row.rest_top - (double)row.top) * (double)a.inv_t);
+        row.rest_top = (float)((double)row.top + ln_rest / a.inv_t64);
+        row.rest_own = (float)exp(ln_rest - ((double)row.rest_top - (double)row.top) * a.inv_t64);
     }
 }
 
@@ -138,13 +141,13 @@ __device__ __forceinline__ float row_loss(const DistillArgs& a, const Part& p, c
     double loss = 0.0;
     if (share != 0.0 && !none)
         loss = share * (p.cross + p.mass * ((p.ref - row.norm) -
-                                             ((double)finite_or_zero(p.near) - (double)row.top) * (double)a.inv_t +
+                                             ((double)finite_or_zero(p.near) - (double)row.top) * a.inv_t64 +
                                              ln_sum));
-    if (p.lost != -INFINITY && exp((double)p.lost * (double)a.inv_t - row.norm) > 0.0) loss += INFINITY;
+    if (p.lost != -INFINITY && exp(over_t(a, p.lost) - row.norm) > 0.0) loss += INFINITY;
     loss = warp_reduce(loss, AddOp());
     if (row.left > 0.0f)
         loss += (double)row.left * (log((double)row.left) - (log((double)row.rest_own) +
-                                                             ((double)row.rest_top - (double)row.top) * (double)a.inv_t - ln_sum));
+                                                             ((double)row.rest_top - (double)row.top) * a.inv_t64 - ln_sum));
     return (float)loss;
 }
 

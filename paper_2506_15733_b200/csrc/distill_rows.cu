@@ -92,7 +92,7 @@ __device__ void list_sums(const DistillArgs& a, int64_t r, const Slice<T>& slice
     }
     warp_maxima(most, near);
     part.near = near;
-    part.ref = a.top_lse ? (double)a.top_lse[r] : (double)most * (double)a.inv_t;
+    part.ref = a.top_lse ? (double)a.top_lse[r] : over_t(a, most);
     part.mass = part.cross = 0.0;
     part.lost = -INFINITY;
     part.listed = 0.0f;
@@ -101,12 +101,12 @@ __device__ void list_sums(const DistillArgs& a, int64_t r, const Slice<T>& slice
         if (missing(ids[j])) continue;
         if (student && a.top_lse && (firsts & 1u)) part.listed += fast_exp2((s.listed_logit[j] - from) * c);
         if (t[j] == -INFINITY) continue;
-        const double x = (double)t[j] * (double)a.inv_t - part.ref, e = exp(x);
+        const double x = over_t(a, t[j]) - part.ref, e = exp(x);
         part.mass += e;
         if (!student || e == 0.0) continue;
         const float logit = s.listed_logit[j];
         if (logit == -INFINITY) part.lost = fmaxf(part.lost, t[j]);
-        else part.cross += e * (x - ((double)logit - (double)from) * (double)a.inv_t);
+        else part.cross += e * (x - ((double)logit - (double)from) * a.inv_t64);
     }
     warp_sums(part.listed, part.mass, part.cross);
     warp_maxima(part.lost);
@@ -291,9 +291,9 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_rows_kernel(const
         float q_id = 0.0f;
         if (s.twice) {
             for (int i = 0; i < a.K; ++i)
-                if (a.top_ids[r * a.K + i] == id) q_id += teacher_q(a.top_values[r * a.K + i], a.inv_t, row.norm);
+                if (a.top_ids[r * a.K + i] == id) q_id += teacher_q(a, a.top_values[r * a.K + i], row.norm);
         } else {
-            q_id = teacher_q(a.top_values[r * a.K + j], a.inv_t, row.norm);
+            q_id = teacher_q(a, a.top_values[r * a.K + j], row.norm);
         }
         grad[id] = Elem<T>::from_float(g.listed(s.listed_logit[j], q_id));
     }

@@ -203,16 +203,16 @@ __device__ void load_list(const DistillArgs& a, int64_t r, Slot& slot, uint32_t*
     warp_maxima(most, near);
     part.near = near;
     near = finite_or_zero(near);
-    part.ref = a.top_lse ? (double)a.top_lse[r] : (double)most * (double)a.inv_t;
+    part.ref = a.top_lse ? (double)a.top_lse[r] : over_t(a, most);
     part.mass = part.cross = 0.0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         if (id[i] < 0 || value[i] == -INFINITY) continue;
-        const double x = (double)value[i] * (double)a.inv_t - part.ref, e = exp(x);
+        const double x = over_t(a, value[i]) - part.ref, e = exp(x);
         part.mass += e;
         if (kMode == kBackward || e == 0.0) continue;
         if (logit[i] == -INFINITY) part.lost = fmaxf(part.lost, value[i]);
-        else part.cross += e * (x - ((double)logit[i] - (double)near) * (double)a.inv_t);
+        else part.cross += e * (x - ((double)logit[i] - (double)near) * a.inv_t64);
     }
     warp_sums(part.mass, part.cross);
     warp_maxima(part.lost);
@@ -241,7 +241,7 @@ __device__ void load_list(const DistillArgs& a, int64_t r, Slot& slot, uint32_t*
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int j = t + i * kListers;
-        const float q = id[i] >= 0 && kMode != kForward ? teacher_q(value[i], a.inv_t, known.norm) : 0.0f;
+        const float q = id[i] >= 0 && kMode != kForward ? teacher_q(a, value[i], known.norm) : 0.0f;
         if (j < a.K) slot.q[j] = q;
         if (id[i] >= 0 && slot.pos[j] < 0) {               // an element of a partial unit
             for (int e = 0; e < 16; ++e)

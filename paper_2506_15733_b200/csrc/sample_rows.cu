@@ -812,7 +812,7 @@ __global__ void __launch_bounds__(kThreads, 2) top_rows_kernel(const TopArgs a) 
     if (c.rank != 0) return;
     if (a.lse && tid >= kThreads - 32) {                     // a warp that has least to do with a short list
         const float ln_sum = log_row_sum(c, s, row, scale);
-        if (tid == kThreads - 1) a.lse[r] = (float)((double)row.top * (double)a.inv_t + (double)ln_sum);
+        if (tid == kThreads - 1) a.lse[r] = (float)((double)row.top * a.inv_t64 + (double)ln_sum);
     }
     if (n > 0) sort_list(n);
     int32_t* ids = a.ids + r * a.K;

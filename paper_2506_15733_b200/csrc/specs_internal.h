@@ -325,14 +325,14 @@ struct SampleArgs {
 };
 struct TopArgs {
     const void* logits; int64_t row_stride, rows; int32_t V, K;
-    float inv_t;
+    float inv_t; double inv_t64;                                                               // rounded once each
     int32_t* ids; float* values; float* lse;                                                   // lse may be NULL
     uint32_t* status; int num_sms;
 };
 struct DistillArgs {
     const void* logits; int64_t row_stride, rows; int32_t V, K;
     const int32_t* top_ids; const float* top_values; const float* top_lse;                     // top_lse may be NULL
-    float inv_t;
+    float inv_t; double inv_t64;                                                               // rounded once each
     const float* row_weight; const float* grad_loss;                                           // may be NULL: 1
     float* loss; float* stats; void* grad; int64_t grad_stride;
     uint32_t* status; int num_sms;

@@ -162,7 +162,7 @@ __device__ __forceinline__ void sum_row(const TopArgs& a, int64_t r, const Strea
     }
     const float most = warp_reduce(top, MaxOp());
     sum = warp_reduce(sum * (top == -INFINITY || top == most ? 1.0f : fast_exp2((top - most) * scale)), AddOp());
-    if (lane == 0) a.lse[r] = (float)((double)most * (double)a.inv_t + (double)logf(sum));
+    if (lane == 0) a.lse[r] = (float)((double)most * a.inv_t64 + (double)logf(sum));
 }
 
 // The team: a key that at least K groups reach, and not many more.  The largest of a thread's groups will do for as many as 5/8
