@@ -178,12 +178,9 @@ struct RunningSums {
 
     __device__ __forceinline__ void raise(float most) {
         if (most > top) {
-            if (top != -INFINITY) {
-                const float scale = fast_exp2((top - most) * c) * ex.mend;
-                rest = __fmul2_rn(rest, make_float2(scale, scale));
-            }
+            const float scale = ex.raise(top, most);
+            if (top != -INFINITY) rest = __fmul2_rn(rest, make_float2(scale, scale));
             top = most;
-            ex = Exponent(top, c);
         }
     }
     // kUnits units, which are changed; flagged(j): unit j may have listed entries, which bits_of(j) then has as a mask.

@@ -282,6 +282,13 @@ struct Exponent {
             out[i] = make_float2(fast_exp2(x.x), fast_exp2(x.y));
         }
     }
+    // Makes the exponents relative to a larger `ref`, and returns what a sum of powers so far has to be multiplied by: it was made
+    // with the old error, and will be put right for the new one.
+    __device__ __forceinline__ float raise(float from, float ref) {
+        const float old = mend;
+        *this = Exponent(ref, c);
+        return fast_exp2((from - ref) * c) * __fdividef(old, mend);
+    }
     __device__ __forceinline__ float operator()(float f) const { return fast_exp2(fmaf(f, c, -offset)); }
     __device__ __forceinline__ float of_logit(float f) const { return operator()(f - shift); }
 };

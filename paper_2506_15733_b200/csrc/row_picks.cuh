@@ -50,12 +50,9 @@ struct GroupMaxima {
     template <int kUnits>
     __device__ __forceinline__ void add_sum(const uint4* q, float most) {
         if (most > top) {
-            if (top != -INFINITY) {
-                const float scale = fast_exp2((top - most) * c) * ex.mend;
-                sums = __fmul2_rn(sums, make_float2(scale, scale));
-            }
+            const float scale = ex.raise(top, most);
+            if (top != -INFINITY) sums = __fmul2_rn(sums, make_float2(scale, scale));
             top = most;
-            ex = Exponent(top, c);
         }
         if (ex.shift == 0.0f) add_powers<kUnits, false>(q);  // (decided here: within the loop it costs 5 instructions a unit)
         else add_powers<kUnits, true>(q);
