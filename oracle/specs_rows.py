@@ -106,10 +106,13 @@ def distill(logits, top_ids, top_values, temperature=1.0, top_lse=None, row_weig
             continue
         t = np.array([t for _, t in here]) / T
         if top_lse is not None:
-            norm = float(np.float32(top_lse[r]))
+            ref, ln_mass = float(np.float32(top_lse[r])), 0.0
         else:
-            norm = t.max() + math.log(np.exp(t - t.max()).sum()) if len(t) and t.max() > -math.inf else math.inf
-        q = np.exp(t - norm) if len(t) else np.zeros(0)
+            # (never added up: next to a lowest value the logarithm would be lost)
+            ref = t.max() if len(t) and t.max() > -math.inf else 0.0
+            mass = np.exp(t - ref).sum()
+            ln_mass = math.log(mass) if mass > 0 else math.inf
+        q = np.exp((t - ref) - ln_mass) if len(t) else np.zeros(0)
         x = logits[r]
         top = float(np.nanmax(x)) if not np.isnan(x).all() else -math.inf
         with np.errstate(invalid="ignore", divide="ignore"):

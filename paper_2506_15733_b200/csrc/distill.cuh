@@ -34,9 +34,9 @@ __device__ __forceinline__ Part no_part() { return {-INFINITY, 0.0f, -INFINITY, 
 __device__ __forceinline__ float finite_or_zero(float v) { return v == -INFINITY ? 0.0f : v; }
 
 // The row's.  Student: the largest logit, the sum over all entries relative to it, and of that the unlisted part (which may have
-// underflowed); the largest unlisted logit, and the sum over the unlisted ones relative to it.  Teacher: norm, the sum of q_j
-// (`listed`), and q_r where it counts (`left`).
-struct Row { float top, sum, rest, rest_top, rest_own, left; double norm, listed; };
+// underflowed); the largest unlisted logit, and the sum over the unlisted ones relative to it.  Teacher: norm = ref + ln_mass (never
+// added up: next to a lowest value the logarithm would be lost), the sum of q_j (`listed`), and q_r where it counts (`left`).
+struct Row { float top, sum, rest, rest_top, rest_own, left; double ref, ln_mass, listed; };
 
 constexpr double kLeastRest = 690.0;                       // exp() of it: 1e-300, well inside the range of a double
 constexpr float kNearRest = 1e-17f;                        // `rest` from here on: fp32 relative to the row's largest logit will do
@@ -45,8 +45,8 @@ constexpr float kNearRest = 1e-17f;                        // `rest` from here o
 __device__ __forceinline__ double over_t(const DistillArgs& a, float v) { return __dmul_rn((double)v, a.inv_t64); }
 
 // q_j for the gradient: the exponent in 64 bits, rounded once.
-__device__ __forceinline__ float teacher_q(const DistillArgs& a, float t, double norm) {
-    return expf((float)(over_t(a, t) - norm));
+__device__ __forceinline__ float teacher_q(const DistillArgs& a, float t, const Row& row) {
+    return expf((float)((over_t(a, t) - row.ref) - row.ln_mass));
 }
 
 // The factor that takes a part's teacher sums to the row's reference.
@@ -57,11 +57,13 @@ __device__ __forceinline__ double teacher_scale(const Part& p, double ref) {
 // The row from sums over all parts.  Teacher:
 __device__ __forceinline__ void set_teacher(const DistillArgs& a, double ref, double mass, Row& row) {
     if (a.top_lse) {
-        row.norm = ref;
+        row.ref = ref;
+        row.ln_mass = 0.0;
         row.listed = mass;
         row.left = (float)fmax(0.0, 1.0 - mass);
     } else {                                               // q sums to 1, or nothing is listed
-        row.norm = mass == 0.0 ? INFINITY : ref + log(mass);
+        row.ref = mass == 0.0 ? 0.0 : ref;
+        row.ln_mass = mass == 0.0 ? INFINITY : log(mass);
         row.listed = mass == 0.0 ? 0.0 : mass != mass ? mass : 1.0;
         row.left = 0.0f;
     }
@@ -137,13 +139,13 @@ __device__ __forceinline__ void student_from_stats(const DistillArgs& a, int64_t
 __device__ __forceinline__ float row_loss(const DistillArgs& a, const Part& p, const Row& row) {
     const double ln_sum = log((double)row.sum);
     const bool none = row.top == -INFINITY && row.sum == 0.0f;      // a student without any entry: all that is listed is lost
-    const double share = p.mass != 0.0 ? exp(p.ref - row.norm) : 0.0;
+    const double ln_share = (p.ref - row.ref) - row.ln_mass, share = p.mass != 0.0 ? exp(ln_share) : 0.0;
     double loss = 0.0;
     if (share != 0.0 && !none)
-        loss = share * (p.cross + p.mass * ((p.ref - row.norm) -
+        loss = share * (p.cross + p.mass * (ln_share -
                                              ((double)finite_or_zero(p.near) - (double)row.top) * a.inv_t64 +
                                              ln_sum));
-    if (p.lost != -INFINITY && exp(over_t(a, p.lost) - row.norm) > 0.0) loss += INFINITY;
+    if (p.lost != -INFINITY && exp((over_t(a, p.lost) - row.ref) - row.ln_mass) > 0.0) loss += INFINITY;
     loss = warp_reduce(loss, AddOp());
     if (row.left > 0.0f)
         loss += (double)row.left * (log((double)row.left) - (log((double)row.rest_own) +

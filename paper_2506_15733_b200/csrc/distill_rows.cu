@@ -291,9 +291,9 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_rows_kernel(const
         float q_id = 0.0f;
         if (s.twice) {
             for (int i = 0; i < a.K; ++i)
-                if (a.top_ids[r * a.K + i] == id) q_id += teacher_q(a, a.top_values[r * a.K + i], row.norm);
+                if (a.top_ids[r * a.K + i] == id) q_id += teacher_q(a, a.top_values[r * a.K + i], row);
         } else {
-            q_id = teacher_q(a, a.top_values[r * a.K + j], row.norm);
+            q_id = teacher_q(a, a.top_values[r * a.K + j], row);
         }
         grad[id] = Elem<T>::from_float(g.listed(s.listed_logit[j], q_id));
     }

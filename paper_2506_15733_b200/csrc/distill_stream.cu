@@ -241,7 +241,7 @@ __device__ void load_list(const DistillArgs& a, int64_t r, Slot& slot, uint32_t*
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int j = t + i * kListers;
-        const float q = id[i] >= 0 && kMode != kForward ? teacher_q(a, value[i], known.norm) : 0.0f;
+        const float q = id[i] >= 0 && kMode != kForward ? teacher_q(a, value[i], known) : 0.0f;
         if (j < a.K) slot.q[j] = q;
         if (id[i] >= 0 && slot.pos[j] < 0) {               // an element of a partial unit
             for (int e = 0; e < 16; ++e)
