@@ -287,7 +287,8 @@ struct Exponent {
     __device__ __forceinline__ float raise(float from, float ref) {
         const float old = mend;
         *this = Exponent(ref, c);
-        return fast_exp2((from - ref) * c) * __fdividef(old, mend);
+        const float d = 1.0f - mend;                        // below 2^-8: 1 / mend = 1 + d + d^2, to 2^-24
+        return fast_exp2((from - ref) * c) * (old * (1.0f + fmaf(d, d, d)));
     }
     __device__ __forceinline__ float operator()(float f) const { return fast_exp2(fmaf(f, c, -offset)); }
     __device__ __forceinline__ float of_logit(float f) const { return operator()(f - shift); }
