@@ -11,8 +11,8 @@
 // the entry leaves it out of its sum (the list warps have those), or writes its gradient after the unit's.
 //
 // Bound: HBM, and the exponentials beside it, which overlap with the copies in part: neither pipe is full.  151936 bf16, 64
-// listed, the remaining mass held against the others: 1024 rows forward 69 us, 4.5 TB/s; backward (152064, 100 listed) 116 us,
-// 5.4 TB/s; 4096 rows step 540 us, 4.6 TB/s.  A gradient whose rows lie otherwise on 16-byte boundaries than the logits' is written
+// listed, the remaining mass held against the others: 1024 rows forward 69 us, 4.5 TB/s; backward (152064, 100 listed) 117 us,
+// 5.4 TB/s; 4096 rows step 535 us, 4.7 TB/s.  A gradient whose rows lie otherwise on 16-byte boundaries than the logits' is written
 // element by element, and that is what bounds it then: 1024 x 151936 bf16, backward 115 -> 371 us, step 145 -> 437 us; 333 x 50021
 // fp32, 31 -> 32 and 45 -> 48 us.
 #include "bulk_ring.cuh"

@@ -6,8 +6,8 @@
 // bounds the K-th largest logit from below; the groups that reach it are read again (from L2), and the entries at or above
 // it, not many more than K, are ranked by counting.  So nobody who streams waits for a pick, and HBM stays busy.
 //
-// Bound: HBM and the exponentials beside it.  1024 x 151936 bf16, K = 64: 69 us, 4.5 TB/s (56 us without the log-sum-exp, which
-// takes an exponential per entry; clusters that stream and pick in turn: 87 us).  fp32 rows of as many bytes: 58 us, 5.3 TB/s.
+// Bound: HBM and the exponentials beside it.  1024 x 151936 bf16, K = 64: 70 us, 4.5 TB/s (56 us without the log-sum-exp, which
+// takes an exponential per entry; clusters that stream and pick in turn: 87 us).  fp32 rows of as many bytes: 59 us, 5.3 TB/s.
 // A pick takes 4 us for K = 64 and 18 us for K = 400, most of it the groups read again while HBM is busy; three teams have
 // three rows' time for it.
 #include <cstddef>
