@@ -408,12 +408,13 @@ int specs_beam_step_fp8(specs_ctx* ctx, const void* hidden, const uint8_t* W_q, 
  *               r * row_stride elements after `logits`; the elements of a row are contiguous.  Any stride (a
  *               padded LM head, 0 for one row read by all) and any alignment that the element type allows.
  *   V           at most SPECS_MAX_ROW_VOCAB, rows at most SPECS_MAX_LOGIT_ROWS (SPECS_ERR_LIMIT).
- * A logit of -inf is a masked entry: it has no probability and is never drawn or listed.  Masks of the
- * type's lowest finite value work too, as the very small numbers they are.  The sampler's masses are whole numbers.
- * Sums of exponentials are fp32 within a warp, and over a CTA's 16 warps in specs_sample_tokens and specs_top_logits;
- * above that they are fp64, as the teacher's sums are throughout.  They are good to about 3e-5 of themselves.  Ids depend on nothing but their row; the number of rows
- * and their alignment decide how a row is shared out, so that a sum's last bit may differ with them.  The same call
- * gives the same bits again. */
+ * A logit of -inf is a masked entry: it has no probability and is never drawn or listed.  Masks of the type's
+ * lowest finite value work too, as the very small numbers they are.  The sampler's masses are whole numbers.
+ * Sums of exponentials are fp32 within a warp, and over a CTA's 16 warps in specs_sample_tokens and
+ * specs_top_logits; above that they are fp64, as the teacher's sums are throughout.  They are good to about
+ * 3e-5 of themselves.  Ids depend on nothing but their row; the number of rows and their alignment decide how
+ * a row is shared out, so that a sum's last bit may differ with them.  The same call gives the same bits
+ * again. */
 #define SPECS_F32  0
 #define SPECS_BF16 1
 #define SPECS_F16  2

@@ -701,7 +701,8 @@ int specs_distill_backward(specs_ctx* ctx, const void* logits, int dtype, int64_
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return SPECS_ERR_CUDA;
     const DistillArgs a = {logits, row_stride, rows, V, K, top_ids, top_values, top_lse, 1.0f / temperature, 1.0 / temperature,
-                           row_weight, grad_loss, nullptr, const_cast<float*>(stats), grad_logits, grad_stride, ctx->d_status, ctx->num_sms};
+                           row_weight, grad_loss, nullptr, const_cast<float*>(stats), grad_logits, grad_stride, ctx->d_status,
+                           ctx->num_sms};
     return launch_distill_backward(a, dtype, static_cast<cudaStream_t>(cuda_stream));
 }
 

@@ -277,7 +277,11 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_rows_kernel(const
         const float loss = row_loss(a, mine, row);
         if (threadIdx.x == kStreamers) {
             a.loss[r] = weight * loss;
-            if (kMode == kForward && a.stats) { a.stats[3 * r] = row.top; a.stats[3 * r + 1] = row.sum; a.stats[3 * r + 2] = rest_to_stats(a, row); }
+            if (kMode == kForward && a.stats) {
+                a.stats[3 * r] = row.top;
+                a.stats[3 * r + 1] = row.sum;
+                a.stats[3 * r + 2] = rest_to_stats(a, row);
+            }
         }
     }
     if (kMode == kForward) return;

@@ -27,7 +27,8 @@ def ctx():
 
 def climbing(g, rows, V, offset, spread):
     """Ascending, descending and shuffled rows around +-offset; row by row a little off it, so that no rounding is favoured."""
-    x = np.sort(g.uniform(0, spread, (rows, V)), axis=1) + (offset * g.uniform(0.97, 1.0, (rows, 1)) * np.where(np.arange(rows) % 2, 1, -1)[:, None])
+    sign = np.where(np.arange(rows) % 2, 1, -1)[:, None]
+    x = np.sort(g.uniform(0, spread, (rows, V)), axis=1) + (offset * g.uniform(0.97, 1.0, (rows, 1)) * sign)
     x[2::3] = g.permuted(x[2::3], axis=1)
     x[1::6] = x[1::6, ::-1]
     return x
